@@ -13,7 +13,8 @@ Every case is one pass as a user of the library makes it.  With `own` set, `run`
 An 8-bit matrix holds e4m3 codes in rows padded with zeros to a multiple of 128 columns, and one power of two
 (e8m0 code) for each block of 1 x 128 or 128 x 128 elements: the smallest one by which the block's largest finite
 magnitude is at most 448.  The scales lie as [column blocks / 4][row blocks][4].  A product sums over the 128
-columns of a block pair and over the blocks.  Clipping multiplies by min(1, max_norm / (norm + 1e-6)).
+columns of a block pair and over the blocks; results in bf16 take the library's fast sums, gradients of
+weights in fp32 its exact ones.  Clipping multiplies by min(1, max_norm / (norm + 1e-6)).
 """
 import torch
 
@@ -276,16 +277,16 @@ def _own_quantize(s, case):
 
 
 def _own_linear(s, case):
-    s["dr"].dr_qlinear(s["x"], s["w"], s["y"], workspace=s["workspace"])
+    s["dr"].dr_qlinear(s["x"], s["w"], s["y"], fast=True, workspace=s["workspace"])
     return s["y"]
 
 
 def _own_train(s, case):
     dr, ws = s["dr"], s["workspace"]
     dr.dr_quantize(s["x"], s["xq"], s["xt"])
-    dr.dr_qmatmul(s["xq"], s["w"], s["y"], workspace=ws)
+    dr.dr_qmatmul(s["xq"], s["w"], s["y"], fast=True, workspace=ws)
     dr.dr_quantize(s["dy"], s["dyq"], s["dyt"])
-    dr.dr_qmatmul(s["dyq"], s["wt"], s["dx"], workspace=ws)
+    dr.dr_qmatmul(s["dyq"], s["wt"], s["dx"], fast=True, workspace=ws)
     dr.dr_qmatmul(s["dyt"], s["xt"], s["dw"], accumulate=case["accumulate"], workspace=ws)
     return {"y": s["y"], "dx": s["dx"], "dw": s["dw"]}
 

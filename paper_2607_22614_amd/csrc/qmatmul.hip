@@ -1,0 +1,208 @@
+// Products of 8-bit matrices (dr_qmatmul, dr_qlinear): c = a * b^T with both operands row-major along K.
+//
+//   c[m, n] = sum over 128-column blocks j of 2^(ea[m, j] + eb[n, j]) * sum over k in block j of qa[m, k] * qb[n, k]
+//
+// b (the weights' side) is the matrix instructions' first operand: a lane then holds four consecutive columns of one
+// row of c.  Which 32 of the 128 columns a lane gives is free as long as both operands agree: lane group g (of four)
+// gives columns 16g.. and 64+16g.., so that each 16-byte load of a wave covers 64 consecutive bytes of 16 rows.
+#include <hip/hip_runtime.h>
+
+#include "quant_device.h"
+
+namespace dr {
+namespace {
+
+struct ProductArgs {
+  QView a, b;
+  const void* x;
+  int64_t x_stride;
+  void* c;
+  int64_t c_stride;
+  uint32_t m, n, kb, tiles_n;
+  int32_t x_vec, c_vec, c_bf16, accumulate;
+};
+
+// 32 codes of a row's 128-column block: p is the row at the block's first column plus 16 * lane group.
+__device__ __forceinline__ i32x8 load_codes(const uint8_t* p) {
+  const u32x4 lo = *reinterpret_cast<const u32x4*>(p), hi = *reinterpret_cast<const u32x4*>(p + 64);
+  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// The 128 columns' share of 16 x 16 outputs with exact products and sums: the values that 32 codes and their scale stand
+// for are exact in bf16, and the bf16 matrix instructions add exact products in fp32.
+struct Bf16Codes {
+  bf16x8 v[4];
+};
+__device__ __forceinline__ Bf16Codes to_bf16(i32x8 codes, int code) {
+  const float scale = __uint_as_float((uint32_t)code << 23);  // the convert takes a power of two by its exponent bits
+  Bf16Codes r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + h], scale, false);
+      const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + h], scale, true);
+      r.v[i][4 * h] = lo[0], r.v[i][4 * h + 1] = lo[1], r.v[i][4 * h + 2] = hi[0], r.v[i][4 * h + 3] = hi[1];
+    }
+  return r;
+}
+__device__ __forceinline__ f32x4 mfma(const Bf16Codes& a, const Bf16Codes& b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], c, 0, 0, 0);
+  return c;
+}
+
+// Columns n0 .. n0+3 of row m of c.
+__device__ __forceinline__ void store4(const ProductArgs& p, uint32_t m, uint32_t n0, f32x4 v) {
+  if (m >= p.m || n0 >= p.n) return;
+  const int64_t at = (int64_t)m * p.c_stride + n0;
+  const bool whole = p.c_vec && n0 + 4 <= p.n;
+  if (p.c_bf16) {
+    uint16_t* c = static_cast<uint16_t*>(p.c) + at;
+    const u32x2 w = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    if (whole) {
+      *reinterpret_cast<u32x2*>(c) = w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n0 + i < p.n) c[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+    }
+  } else {
+    float* c = static_cast<float*>(p.c) + at;
+    if (whole) {
+      f32x4* q = reinterpret_cast<f32x4*>(c);
+      *q = p.accumulate ? *q + v : v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n0 + i < p.n) c[i] = p.accumulate ? c[i] + v[i] : v[i];
+    }
+  }
+}
+
+// Codes and scale of 128 columns of one row of x, quantized as dr_quantize does; each lane holds 32 of them.
+template <bool BF16>
+__device__ __forceinline__ i32x8 quantize_block(const ProductArgs& p, uint32_t row, uint32_t col, int& code) {
+  float v[4][8];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t c = col + (q >> 1) * 64 + (q & 1) * 8;
+    load8<BF16>(p.x, (int64_t)row * p.x_stride + c, max(0, min(8, (int)p.a.cols - (int)c)), p.x_vec, v[q]);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) m = max(m, abs_bits(v[i / 8][i % 8]));
+  m = max_rows(m);
+  const bool odd = __any(m >= kInfBits);
+  if (odd) {
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, finite_bits(v[i / 8][i % 8]));
+    m = max_rows(m);
+  }
+  code = (int)scale_code(m);
+  const float inv = inverse_scale((uint32_t)code);
+  i32x8 w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float* f = &v[i / 2][(i % 2) * 4];
+    w[i] = (int)(odd ? to_e4m3<true>(f[0], f[1], f[2], f[3], inv) : to_e4m3<false>(f[0], f[1], f[2], f[3], inv));
+  }
+  return w;
+}
+
+// Scale code of block column j for the lane's block row.
+__device__ __forceinline__ int load_code(const QView& q, uint32_t row, uint32_t j) {
+  return q.scales[((int64_t)(j >> 2) * q.srows + (row >> q.sh)) * 4 + (j & 3)];
+}
+
+// A tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
+// instructions; the KS waves of the workgroup take the 128-column blocks in turn and join their sums in LDS, in the
+// order of the waves.  X: 0 takes a from its codes, 1 quantizes fp32 rows of x, 2 bf16 rows.
+template <int FT, int TT, int KS, int X>
+__global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) {
+  __shared__ f32x4 part[KS][FT * TT][64];
+  const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t n0 = blockIdx.x % p.tiles_n * (FT * 16), m0 = blockIdx.x / p.tiles_n * (TT * 16);
+  const uint8_t *bp[FT], *ap[TT];
+  uint32_t brow[FT], arow[TT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f) {
+    brow[f] = min(n0 + f * 16 + r, p.n - 1);
+    bp[f] = p.b.data + (int64_t)brow[f] * p.b.stride + g * 16;
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    arow[t] = min(m0 + t * 16 + r, p.m - 1);
+    ap[t] = p.a.data + (int64_t)arow[t] * p.a.stride + g * 16;
+  }
+  f32x4 acc[FT][TT] = {};
+  for (uint32_t j = wave; j < p.kb; j += KS) {
+    Bf16Codes bw[FT], aw[TT];
+#pragma unroll
+    for (int f = 0; f < FT; ++f) {
+      bw[f] = to_bf16(load_codes(bp[f] + (int64_t)j * 128), load_code(p.b, brow[f], j));
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      if (X == 0) {
+        aw[t] = to_bf16(load_codes(ap[t] + (int64_t)j * 128), load_code(p.a, arow[t], j));
+      } else {
+        int code;
+        const i32x8 w = quantize_block<X == 2>(p, arow[t], j * 128 + g * 16, code);
+        aw[t] = to_bf16(w, code);
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int t = 0; t < TT; ++t) acc[f][t] = mfma(bw[f], aw[t], acc[f][t]);
+  }
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) part[wave][f * TT + t][lane] = acc[f][t];
+  __syncthreads();
+  for (uint32_t i = wave; i < FT * TT; i += KS) {
+    f32x4 s = part[0][i][lane];
+#pragma unroll
+    for (int k = 1; k < KS; ++k) s += part[k][i][lane];
+    store4(p, m0 + i % TT * 16 + r, n0 + i / TT * 16 + g * 4, s);
+  }
+}
+
+template <int FT, int TT, int KS, int X>
+void launch_direct(ProductArgs a, hipStream_t st) {
+  a.tiles_n = (uint32_t)ceil_div(a.n, FT * 16);
+  const uint32_t grid = a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16);
+  hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), dim3(grid), dim3(64 * KS), 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
+  ProductArgs a;
+  a.a = l.a;
+  a.b = l.b;
+  a.x = l.x;
+  a.x_stride = l.x_stride;
+  a.c = l.c;
+  a.c_stride = l.c_stride;
+  a.m = l.m;
+  a.n = l.n;
+  a.kb = l.kb;
+  a.x_vec = l.x_aligned;
+  a.c_vec = reinterpret_cast<uintptr_t>(l.c) % (l.c_bf16 ? 8 : 16) == 0 && l.c_stride % 4 == 0;
+  a.c_bf16 = l.c_bf16;
+  a.accumulate = l.accumulate;
+  if (l.x) {
+    if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, st);
+    else launch_direct<1, 1, 8, 1>(a, st);
+  } else {
+    launch_direct<2, 4, 4, 0>(a, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace dr

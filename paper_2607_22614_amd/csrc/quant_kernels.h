@@ -1,0 +1,54 @@
+// Launches of the 8-bit kernels (quantize.hip, qmatmul.hip) and of the gradient kernels
+// (grad_clip.hip): plain arguments, checked by the host code that fills them (quant.cpp,
+// grads.cpp).  Each wrapper enqueues on `st` and returns hipGetLastError().
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "dr.h"
+
+namespace dr {
+
+constexpr int64_t kBlock = DR_QUANT_BLOCK;
+constexpr int64_t kMaxQRows = 1ll << 26;  // exclusive: 16 rows a workgroup of 512 lanes is 2^31 lanes
+constexpr int64_t kMaxQCols = 1ll << 23;  // 256 rows of a tile lie within 2^31 bytes
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// One operand as the kernels see it; sh: log2 of block_rows, srows: block rows.
+struct QView {
+  uint8_t* data;
+  uint8_t* scales;
+  int64_t stride;
+  uint32_t rows, cols, srows;
+  int32_t sh;
+};
+
+struct QuantizeLaunch {
+  const void* src;
+  int64_t src_stride;  // elements
+  uint32_t rows, cols;
+  bool bf16, aligned;  // aligned: 16-byte aligned rows
+  QView q, qt;         // data null: not wanted
+};
+hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st);
+
+// c (m x n) = a (m x k) * b^T (n x k), kb = ceil(k / 128) column blocks.
+struct ProductLaunch {
+  QView a, b;
+  const void* x;     // set: a is quantized in the kernel from these rows
+  int64_t x_stride;  // elements
+  bool x_bf16, x_aligned;
+  void* c;
+  int64_t c_stride;  // elements
+  uint32_t m, n, kb;
+  bool c_bf16, accumulate, fast;
+  void* workspace;
+};
+hipError_t launch_product(const ProductLaunch& l, hipStream_t st);
+// Rows that launch_product quantizes itself.
+constexpr uint32_t kFusedRows = 16;
+
+}  // namespace dr

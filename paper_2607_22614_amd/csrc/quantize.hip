@@ -1,0 +1,239 @@
+// Quantization to e4m3 codes with a power of two for each block of 128 columns (dr_quantize).
+//
+// With amax the largest finite magnitude of a block, its scale is 2^e with e = ceil(log2(amax / 448)) and an
+// element's code is x * 2^-e rounded to 4 significant bits.  Both multiplications by powers of two are
+// exact, so the codes depend on nothing but the definition.
+//
+// HBM-bound: 2 or 4 bytes read and 1 byte written per element and orientation.
+#include <hip/hip_runtime.h>
+
+#include "quant_device.h"
+
+namespace dr {
+namespace {
+
+struct QuantizeArgs {
+  const void* src;
+  int64_t src_stride;
+  uint32_t rows, cols, tiles_x;
+  int32_t vec;
+  QView q, qt;
+};
+
+// Blocks of 1 x 128, rows only.  A wave takes 512 columns (four blocks, 16 lanes each, 8 elements a lane) of
+// kRowsPerWave rows, whose loads are all in flight together; a block's maximum is a DPP reduction over its 16
+// lanes, and the four codes of a row make the 32-bit word that one lane stores.
+constexpr int kRowsPerWave = 8;
+constexpr int kRowWaves = 4;
+
+template <bool BF16>
+__global__ __launch_bounds__(64 * kRowWaves) void quantize_rows_kernel(QuantizeArgs a) {
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const uint32_t quad = blockIdx.x % a.tiles_x;
+  const uint32_t row0 = (blockIdx.x / a.tiles_x * kRowWaves + wave) * kRowsPerWave;
+  if (row0 >= a.rows) return;
+  const uint32_t col = quad * 512 + lane * 8;
+  const int n = max(0, min(8, (int)a.cols - (int)col));
+  float v[kRowsPerWave][8];
+#pragma unroll
+  for (int i = 0; i < kRowsPerWave; ++i)
+    load8<BF16>(a.src, (int64_t)min(row0 + i, a.rows - 1) * a.src_stride + col, n, a.vec, v[i]);
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < kRowsPerWave; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i][j]));
+    m = max16(m);
+    const bool odd = __any(m >= kInfBits);
+    if (odd) {
+      m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = max(m, finite_bits(v[i][j]));
+      m = max16(m);
+    }
+    const uint32_t code = scale_code(m);
+    const float inv = inverse_scale(code);
+    u32x2 w;
+    if (odd) {
+      w = u32x2{to_e4m3<true>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<true>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+    } else {
+      w = u32x2{to_e4m3<false>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<false>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+    }
+    const uint32_t codes = (uint32_t)__builtin_amdgcn_readlane((int)code, 0) | (uint32_t)__builtin_amdgcn_readlane((int)code, 16) << 8 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)code, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)code, 48) << 24;
+    if ((int)lane == i) word = codes;
+    if (row0 + i < a.rows && (col & ~127u) < a.cols)
+      *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = w;
+  }
+  if (lane < kRowsPerWave && row0 + lane < a.rows)
+    reinterpret_cast<uint32_t*>(a.q.scales)[(int64_t)quad * a.rows + row0 + lane] = word;
+}
+
+// Scale code of block (i, j) of a matrix with R block rows, and 127 in the unused bytes of its last word.
+__device__ __forceinline__ void put_code(const QView& q, uint32_t i, uint32_t j, uint32_t code) {
+  const uint32_t blocks = (q.cols + 127) / 128;
+  uint8_t* p = q.scales + ((int64_t)(j >> 2) * q.srows + i) * 4;
+  p[j & 3] = (uint8_t)code;
+  if (j + 1 == blocks)
+    for (uint32_t k = (j & 3) + 1; k < 4; ++k) p[k] = 127;
+}
+
+// A tile of 128 x 128 per workgroup, each lane 8 columns of 8 rows, kept in registers.  ROWS writes the codes
+// along the rows, COLS the transpose: its codes are packed 8 rows to a word, turned in LDS (one 128-byte row per
+// column, 8-byte pieces spread by an exclusive or so that a wave's stores meet no bank twice), and leave as whole
+// 128-byte rows.  SQUARE: one scale for the tile, else one per row (DPP) and one per column (over the four rows of
+// lanes, then over the waves in LDS).
+template <bool BF16, bool SQUARE, bool ROWS, bool COLS>
+__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
+  __shared__ uint32_t cmax[4][128];
+  __shared__ __align__(16) uint8_t turned[COLS ? 128 * 128 : 16];
+  const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;
+  const uint32_t ct = blockIdx.x % a.tiles_x, rt = blockIdx.x / a.tiles_x;
+  const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * 8;
+  const int n = max(0, min(8, (int)a.cols - (int)col));
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool in = row0 + i < a.rows;
+    load8<BF16>(a.src, (int64_t)(in ? row0 + i : a.rows - 1) * a.src_stride + col, in ? n : 0, a.vec, v[i]);
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[i][j]));
+  const bool odd = __any(top >= kInfBits);
+
+  uint32_t square_code = 0;
+  if (SQUARE) {
+    uint32_t m = top;
+    if (odd) {
+      m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, finite_bits(v[i][j]));
+    }
+    m = max_rows(max16(m));
+    if ((tid & 63) == 0) cmax[0][wave] = m;
+    __syncthreads();
+    square_code = scale_code(max(max(cmax[0][0], cmax[0][1]), max(cmax[0][2], cmax[0][3])));
+    if (tid == 0) {
+      if (ROWS) put_code(a.q, rt, ct, square_code);
+      if (COLS) put_code(a.qt, ct, rt, square_code);
+    }
+  }
+
+  if (ROWS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t code = square_code;
+      if (!SQUARE) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, odd ? finite_bits(v[i][j]) : abs_bits(v[i][j]));
+        code = scale_code(max16(m));
+      }
+      const float inv = inverse_scale(code);
+      u32x2 w;
+      if (odd)
+        w = u32x2{to_e4m3<true>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<true>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+      else
+        w = u32x2{to_e4m3<false>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<false>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+      if (row0 + i < a.rows) {
+        *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = w;
+        if (!SQUARE && tx == 0) put_code(a.q, row0 + i, ct, code);
+      }
+    }
+  }
+
+  if (COLS) {
+    uint32_t code[8];
+    if (SQUARE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) code[j] = square_code;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, odd ? finite_bits(v[i][j]) : abs_bits(v[i][j]));
+        m = max_rows(m);
+        if ((tid & 63) < 16) cmax[wave][tx * 8 + j] = m;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t c = tx * 8 + j;
+        code[j] = scale_code(max(max(cmax[0][c], cmax[1][c]), max(cmax[2][c], cmax[3][c])));
+        if (ty == 0 && ct * 128 + c < a.cols) put_code(a.qt, ct * 128 + c, rt, code[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float inv = inverse_scale(code[j]);
+      u32x2 w;
+      if (odd)
+        w = u32x2{to_e4m3<true>(v[0][j], v[1][j], v[2][j], v[3][j], inv), to_e4m3<true>(v[4][j], v[5][j], v[6][j], v[7][j], inv)};
+      else
+        w = u32x2{to_e4m3<false>(v[0][j], v[1][j], v[2][j], v[3][j], inv), to_e4m3<false>(v[4][j], v[5][j], v[6][j], v[7][j], inv)};
+      *reinterpret_cast<u32x2*>(turned + (tx * 8 + j) * 128 + ((ty ^ tx) * 8)) = w;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t c = r * 32 + tid / 8, piece = tid % 8, x = c / 8;
+      // pieces 2p and 2p+1 lie at (2p)^x and (2p+1)^x: side by side, in turned order where x is odd
+      u32x4 w = *reinterpret_cast<const u32x4*>(turned + c * 128 + ((2 * piece) ^ (x & ~1u)) * 8);
+      if (x & 1) w = u32x4{w[2], w[3], w[0], w[1]};
+      if (ct * 128 + c < a.cols)
+        *reinterpret_cast<u32x4*>(a.qt.data + (int64_t)(ct * 128 + c) * a.qt.stride + rt * 128 + piece * 16) = w;
+    }
+  }
+}
+
+template <bool BF16, bool SQUARE>
+void launch_tiles(const QuantizeArgs& a, dim3 grid, hipStream_t st) {
+  if (a.q.data && a.qt.data)
+    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, true>), grid, dim3(256), 0, st, a);
+  else if (a.q.data)
+    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, false>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, false, true>), grid, dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
+  QuantizeArgs a;
+  a.src = l.src;
+  a.src_stride = l.src_stride;
+  a.rows = l.rows;
+  a.cols = l.cols;
+  a.vec = l.aligned;
+  a.q = l.q;
+  a.qt = l.qt;
+  const bool square = (l.q.data ? l.q.sh : l.qt.sh) != 0;
+  if (!square && !l.qt.data) {
+    a.tiles_x = (uint32_t)ceil_div(l.cols, 512);
+    const uint32_t grid = a.tiles_x * (uint32_t)ceil_div(l.rows, kRowsPerWave * kRowWaves);
+    if (l.bf16)
+      hipLaunchKernelGGL(quantize_rows_kernel<true>, dim3(grid), dim3(64 * kRowWaves), 0, st, a);
+    else
+      hipLaunchKernelGGL(quantize_rows_kernel<false>, dim3(grid), dim3(64 * kRowWaves), 0, st, a);
+    return hipGetLastError();
+  }
+  a.tiles_x = (uint32_t)ceil_div(l.cols, 128);
+  const dim3 grid(a.tiles_x * (uint32_t)ceil_div(l.rows, 128));
+  if (l.bf16) {
+    if (square) launch_tiles<true, true>(a, grid, st);
+    else launch_tiles<true, false>(a, grid, st);
+  } else {
+    if (square) launch_tiles<false, true>(a, grid, st);
+    else launch_tiles<false, false>(a, grid, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace dr

@@ -88,11 +88,26 @@ class dr_hyst_decision(ctypes.Structure):
                 ("run", ctypes.c_int32), ("imbalance", ctypes.c_double), ("predicted_gain_s", ctypes.c_double)]
 
 
+class dr_qmatrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("stride", ctypes.c_int64), ("block_rows", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class dr_grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("grad_type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+DR_TYPE_F32, DR_TYPE_BF16 = 0, 1
+DR_QUANT_BLOCK = 128
+DR_ACCUMULATE, DR_FAST_SUMS = 1, 2
 DR_HYST_BALANCED, DR_HYST_PERSISTENCE, DR_HYST_COOLDOWN, DR_HYST_DWELL, DR_HYST_EDGE, DR_HYST_AMORTIZE, \
     DR_HYST_RESIZE = range(7)
 
 _P = ctypes.c_void_p
 _PP = ctypes.POINTER(ctypes.c_void_p)
+_I64, _PU64, _PQ = ctypes.c_int64, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(dr_qmatrix)
 _SIGS = {
     "dr_plan_create": ([ctypes.POINTER(dr_model), ctypes.POINTER(dr_layout), ctypes.POINTER(_P)], ctypes.c_int),
     "dr_plan_create_host": ([ctypes.POINTER(dr_model), ctypes.POINTER(dr_layout), ctypes.POINTER(_P)], ctypes.c_int),
@@ -121,6 +136,17 @@ _SIGS = {
     "dr_hyst_step": ([_P, ctypes.c_double, ctypes.c_double, ctypes.POINTER(dr_hyst_decision)], ctypes.c_int),
     "dr_hyst_destroy": ([_P], None),
     "dr_break_even_steps": ([ctypes.c_double, ctypes.c_double, ctypes.c_double], ctypes.c_double),
+    "dr_qmatrix_sizes": ([_I64, _I64, ctypes.c_int32, ctypes.POINTER(_I64), _PU64, _PU64], ctypes.c_int),
+    "dr_quantize": ([_P, ctypes.c_int32, _I64, _I64, _I64, _PQ, _PQ, _P], ctypes.c_int),
+    "dr_qmatmul": ([_PQ, _PQ, _P, ctypes.c_int32, _I64, ctypes.c_int32, _P, ctypes.c_uint64, _P], ctypes.c_int),
+    "dr_qmatmul_workspace": ([_I64, _I64, _I64, _PU64], ctypes.c_int),
+    "dr_qlinear": ([_P, ctypes.c_int32, _I64, _I64, _PQ, _P, ctypes.c_int32, _I64, ctypes.c_int32, _P,
+                    ctypes.c_uint64, _P], ctypes.c_int),
+    "dr_qlinear_workspace": ([_I64, _I64, _I64, _PU64], ctypes.c_int),
+    "dr_grad_workspace": ([_PU64], ctypes.c_int),
+    "dr_grad_norm": ([ctypes.POINTER(dr_grad), _I64, _P, _P, _P, _P], ctypes.c_int),
+    "dr_grad_scale": ([ctypes.POINTER(dr_grad), _I64, _P, ctypes.c_double, _P, _P], ctypes.c_int),
+    "dr_grad_clip": ([ctypes.POINTER(dr_grad), _I64, ctypes.c_double, _P, _P, _P], ctypes.c_int),
     "dr_last_error": ([], ctypes.c_char_p),
 }
 for _name, (_args, _res) in _SIGS.items():
@@ -497,6 +523,174 @@ def dr_hyst_step(h: Hysteresis, t_rollout: float, t_train: float) -> dict:
 
 def dr_break_even_steps(switch_cost_s: float, step_before_s: float, step_after_s: float) -> float:
     return _lib.dr_break_even_steps(float(switch_cost_s), float(step_before_s), float(step_after_s))
+
+
+# ------------------------------------------------------------------ 8-bit matrices
+def _type(t, where: str) -> int:
+    """DR_TYPE_* of a tensor."""
+    import torch
+    if t.dtype is torch.bfloat16:
+        return DR_TYPE_BF16
+    if t.dtype is torch.float32:
+        return DR_TYPE_F32
+    raise ValueError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+
+
+def _dense_rows(t, where: str):
+    """(address, type, rows, cols, row stride) of a 2-d device tensor whose rows are dense."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{where}: expected a 2-d device tensor, got {t.dim()}-d on {t.device}")
+    rows, cols = t.shape
+    step, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{where}: the elements of a row are not adjacent")
+    if step < cols and rows > 1:
+        raise ValueError(f"{where}: rows overlap")
+    return t.data_ptr(), _type(t, where), rows, cols, step if rows > 1 else max(step, cols)
+
+
+def dr_qmatrix_sizes(rows: int, cols: int, block_rows: int = 1) -> dict:
+    """{"stride", "data_bytes", "scale_bytes"} of a rows x cols 8-bit matrix."""
+    stride, data, scales = ctypes.c_int64(), ctypes.c_uint64(), ctypes.c_uint64()
+    _check(_lib.dr_qmatrix_sizes(int(rows), int(cols), int(block_rows), ctypes.byref(stride), ctypes.byref(data),
+                                 ctypes.byref(scales)), "dr_qmatrix_sizes")
+    return {"stride": stride.value, "data_bytes": data.value, "scale_bytes": scales.value}
+
+
+class QMatrix:
+    """An 8-bit matrix over two device tensors of one-byte elements, which it keeps: data [rows, at least
+    cols rounded up to 128] with dense rows, and scales (dense, [ceil(ceil(cols/128)/4), block rows, 4])."""
+
+    __slots__ = ("data", "scales", "rows", "cols", "block_rows", "c", "ref")
+
+    def __init__(self, data, scales, rows: int, cols: int, block_rows: int = 1):
+        need = dr_qmatrix_sizes(rows, cols, block_rows)
+        if data.element_size() != 1 or scales.element_size() != 1 or not data.is_cuda or not scales.is_cuda:
+            raise ValueError("QMatrix: data and scales are device tensors of one-byte elements")
+        if data.dim() != 2 or data.shape[0] != rows or data.shape[1] < need["stride"] or data.stride(1) != 1:
+            raise ValueError(f"QMatrix: data is not [{rows}, at least {need['stride']}] with dense rows")
+        if not scales.is_contiguous() or scales.numel() < need["scale_bytes"]:
+            raise ValueError(f"QMatrix: scales are not {need['scale_bytes']} dense bytes")
+        stride = data.stride(0) if rows > 1 and cols else need["stride"]
+        if stride < need["stride"]:
+            raise ValueError("QMatrix: rows overlap")
+        self.data, self.scales, self.rows, self.cols, self.block_rows = data, scales, int(rows), int(cols), int(block_rows)
+        self.c = dr_qmatrix(data.data_ptr(), scales.data_ptr(), self.rows, self.cols, stride, self.block_rows, 0)
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "QMatrix":
+        import torch
+        stride = dr_qmatrix_sizes(rows, cols, block_rows)["stride"]
+        words, block = -(-stride // (4 * DR_QUANT_BLOCK)), -(-rows // block_rows)
+        return cls(torch.empty((rows, stride), dtype=torch.uint8, device=device),
+                   torch.empty((words, block, 4), dtype=torch.uint8, device=device), rows, cols, block_rows)
+
+
+def dr_quantize(src, q: QMatrix | None = None, qt: QMatrix | None = None, stream=None) -> None:
+    """src (2-d float32 or bfloat16) to 8 bits: as it is into q, transposed into qt."""
+    addr, kind, rows, cols, step = _dense_rows(src, "dr_quantize src")
+    _check(_lib.dr_quantize(addr, kind, rows, cols, step, q.ref if q else None, qt.ref if qt else None,
+                            _stream(stream)), "dr_quantize")
+
+
+def _workspace(ws, where: str):
+    """(address, bytes) of a workspace tensor or None."""
+    if ws is None:
+        return 0, 0
+    return (ws.data_ptr() if _fits(ws, 0) else _buf(ws, 0, where, True)), ws.nbytes
+
+
+def dr_qmatmul(a: QMatrix, b: QMatrix, out, accumulate: bool = False, fast: bool = False, workspace=None,
+               stream=None) -> None:
+    """out = a b^T (+= with accumulate), out 2-d float32 or bfloat16; fast: DR_FAST_SUMS."""
+    addr, kind, rows, cols, step = _dense_rows(out, "dr_qmatmul out")
+    if rows != a.rows or cols != b.rows:
+        raise ValueError(f"dr_qmatmul out: {rows} x {cols}, the product is {a.rows} x {b.rows}")
+    _check(_lib.dr_qmatmul(a.ref, b.ref, addr, kind, step,
+                           (DR_ACCUMULATE if accumulate else 0) | (DR_FAST_SUMS if fast else 0),
+                           *_workspace(workspace, "dr_qmatmul workspace"), _stream(stream)), "dr_qmatmul")
+
+
+def _bytes(call, where: str, *args) -> int:
+    n = ctypes.c_uint64()
+    _check(call(*args, ctypes.byref(n)), where)
+    return n.value
+
+
+def dr_qmatmul_workspace(m: int, n: int, k: int) -> int:
+    """Bytes of workspace that an m x n product over k columns needs."""
+    return _bytes(_lib.dr_qmatmul_workspace, "dr_qmatmul_workspace", int(m), int(n), int(k))
+
+
+def dr_qlinear(x, w: QMatrix, out, fast: bool = False, workspace=None, stream=None) -> None:
+    """out = x w^T with x (2-d float32 or bfloat16) quantized in blocks of 1 x 128; fast: DR_FAST_SUMS."""
+    addr, kind, rows, cols, step = _dense_rows(x, "dr_qlinear x")
+    oaddr, okind, orows, ocols, ostep = _dense_rows(out, "dr_qlinear out")
+    if cols != w.cols or orows != rows or ocols != w.rows:
+        raise ValueError(f"dr_qlinear: x {rows} x {cols}, w {w.rows} x {w.cols}, out {orows} x {ocols}")
+    _check(_lib.dr_qlinear(addr, kind, rows, step, w.ref, oaddr, okind, ostep, DR_FAST_SUMS if fast else 0,
+                           *_workspace(workspace, "dr_qlinear workspace"), _stream(stream)), "dr_qlinear")
+
+
+def dr_qlinear_workspace(m: int, w: QMatrix) -> int:
+    """Bytes of workspace that dr_qlinear needs for m rows and these weights."""
+    return _bytes(_lib.dr_qlinear_workspace, "dr_qlinear_workspace", int(m), w.rows, w.cols)
+
+
+# ------------------------------------------------------------------ gradients
+class GradList:
+    """The gradients of a model and where their scaled values go (outs None: in place), any shapes: the list that
+    the dr_grad_* calls take.  Keeps the tensors."""
+
+    __slots__ = ("grads", "outs", "c", "count")
+
+    def __init__(self, grads: Sequence, outs: Sequence | None = None):
+        self.grads, self.outs = tuple(grads), tuple(grads if outs is None else outs)
+        if len(self.outs) != len(self.grads):
+            raise ValueError(f"GradList: {len(self.grads)} gradients, {len(self.outs)} outputs")
+        self.count = len(self.grads)
+        self.c = (dr_grad * max(self.count, 1))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            for t in (g, o):
+                if not t.is_cuda or not t.is_contiguous():
+                    raise ValueError(f"GradList[{i}]: expected a dense device tensor")
+            if g.numel() != o.numel():
+                raise ValueError(f"GradList[{i}]: {g.numel()} elements to {o.numel()}")
+            self.c[i] = dr_grad(g.data_ptr(), o.data_ptr(), g.numel(), _type(g, f"GradList[{i}]"),
+                                _type(o, f"GradList[{i}]"))
+
+
+def dr_grad_workspace() -> int:
+    """Bytes of workspace that dr_grad_norm and dr_grad_clip need."""
+    return _bytes(_lib.dr_grad_workspace, "dr_grad_workspace")
+
+
+_GRAD_WORKSPACE = dr_grad_workspace()
+
+
+def _grad_space(ws, where: str) -> int:
+    return _buf(ws, _GRAD_WORKSPACE, where, True)
+
+
+def dr_grad_norm(grads: GradList, workspace, sum_squares=None, norm=None, stream=None) -> None:
+    """sum_squares (one float64) and norm (one float32) of all gradients, on the device."""
+    _check(_lib.dr_grad_norm(grads.c, grads.count, _grad_space(workspace, "dr_grad_norm workspace"),
+                             _buf(sum_squares, 8, "dr_grad_norm sum_squares", True),
+                             _buf(norm, 4, "dr_grad_norm norm", True), _stream(stream)), "dr_grad_norm")
+
+
+def dr_grad_scale(grads: GradList, sum_squares, max_norm: float, norm_out=None, stream=None) -> None:
+    """Every gradient times min(1, max_norm / (norm + 1e-6)), with the norm of sum_squares (one float64)."""
+    _check(_lib.dr_grad_scale(grads.c, grads.count, _buf(sum_squares, 8, "dr_grad_scale sum_squares", True),
+                              float(max_norm), _buf(norm_out, 4, "dr_grad_scale norm_out", True), _stream(stream)),
+           "dr_grad_scale")
+
+
+def dr_grad_clip(grads: GradList, max_norm: float, norm_out, workspace, stream=None) -> None:
+    """dr_grad_norm and dr_grad_scale in one call; norm_out may be None."""
+    _check(_lib.dr_grad_clip(grads.c, grads.count, float(max_norm), _grad_space(workspace, "dr_grad_clip workspace"),
+                             _buf(norm_out, 4, "dr_grad_clip norm_out", True), _stream(stream)), "dr_grad_clip")
 
 
 def dr_last_error() -> str:

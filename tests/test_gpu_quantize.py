@@ -1,0 +1,122 @@
+"""dr_quantize on the GPU: codes and scales equal to the oracle's, byte for byte."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import quant
+from tests.gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+
+POISON = 0xA5
+
+
+def _dr():
+    from paper_2607_22614_amd import dr
+    return dr
+
+
+def _input(rows, cols, dtype, seed=0, specials=True):
+    """Values over many magnitudes; zero blocks, values that are not finite, subnormals and scales' edges among them."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * 2.0**rng.integers(-6, 6, (rows, cols)) * 2.0**rng.integers(-30, 30, (rows, 1))
+    if specials:
+        flat = x.reshape(-1)
+        at = rng.permutation(flat.size)[:max(1, flat.size // 50)]
+        flat[at] = rng.choice([np.nan, np.inf, -np.inf, 0.0, -0.0, 448.0, 449.0, 447.9, 3e38, 1e-40, -1e-45, 2.0**-126, 2.0**-119], at.size)
+        x[rows // 2, :] = 0.0
+        if rows > 4:
+            x[rows // 3, :] = np.nan
+            x[rows // 4, :] = rng.choice([1e-41, -3e-39, 2.0**-130], cols)
+    t = torch.from_numpy(x.astype(np.float32))
+    return t.to(torch.bfloat16) if dtype == "bf16" else t
+
+
+def _poisoned(dr, rows, cols, block_rows, extra=0):
+    m = dr.QMatrix.empty(rows, cols, block_rows)
+    wide = torch.full((rows + 1, m.data.shape[1] + extra), POISON, dtype=torch.uint8, device="cuda")
+    scales = torch.full((m.scales.numel() + 16,), POISON, dtype=torch.uint8, device="cuda")
+    q = dr.QMatrix(wide[:rows], scales[:m.scales.numel()].view(m.scales.shape), rows, cols, block_rows)
+    return q, wide, scales
+
+
+def _check(q, wide, scales, want):
+    codes, sc = want
+    rows, padded = codes.shape
+    got = wide.cpu().numpy()
+    both_nan = ((codes & 0x7F) == 0x7F) & ((got[:rows, :padded] & 0x7F) == 0x7F)
+    assert np.array_equal(np.where(both_nan, codes, got[:rows, :padded]), codes)
+    assert (got[rows:] == POISON).all() and (got[:, padded:] == POISON).all(), "written outside the matrix"
+    got = scales.cpu().numpy()
+    assert np.array_equal(got[:sc.size], sc.reshape(-1)) and (got[sc.size:] == POISON).all()
+
+
+SHAPES = [(1, 1), (1, 128), (2, 129), (5, 8), (128, 128), (129, 127), (333, 344), (40, 1100), (300, 512), (257, 513)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("which", ["q", "qt", "both"])
+def test_codes_and_scales(rows, cols, dtype, block_rows, which):
+    dr = _dr()
+    say("quantize", rows, cols, dtype, block_rows, which)
+    x = _input(rows, cols, dtype, rows * 1000 + cols)
+    ref = x.to(torch.float64).numpy()
+    q = _poisoned(dr, rows, cols, block_rows, 16) if which != "qt" else None
+    qt = _poisoned(dr, cols, rows, block_rows, 16) if which != "q" else None
+    dr.dr_quantize(x.cuda(), q[0] if q else None, qt[0] if qt else None)
+    torch.cuda.synchronize()
+    if q:
+        _check(*q, quant.quantize(ref, block_rows))
+    if qt:
+        _check(*qt, quant.quantize(ref.T, block_rows))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset,stride", [(1, 301), (8, 304), (3, 512)])
+def test_rows_at_any_element(dtype, offset, stride):
+    dr = _dr()
+    say("strided rows", dtype, offset, stride)
+    rows, cols = 70, 300
+    x = _input(rows, cols, dtype, 7)
+    buf = torch.full((offset + rows * stride,), float("nan"), dtype=x.dtype, device="cuda")
+    src = buf[offset:].view(rows, stride)[:, :cols]
+    src.copy_(x)
+    for block_rows in (1, 128):
+        q, qt = _poisoned(dr, rows, cols, block_rows), _poisoned(dr, cols, rows, block_rows)
+        dr.dr_quantize(src, q[0], qt[0])
+        one = _poisoned(dr, rows, cols, block_rows)
+        dr.dr_quantize(src, one[0])
+        torch.cuda.synchronize()
+        ref = x.to(torch.float64).numpy()
+        _check(*q, quant.quantize(ref, block_rows))
+        _check(*one, quant.quantize(ref, block_rows))
+        _check(*qt, quant.quantize(ref.T, block_rows))
+
+
+@pytest.mark.parametrize("top", [2.0**-140, 1e-30, 1.0, 447.0, 448.0, 448.5, 3.0e38])
+def test_every_bf16_pattern(top):
+    """All 2^16 patterns below `top`, in blocks whose maximum is `top`: every rounding, at several scales."""
+    dr = _dr()
+    say("every bf16 pattern", top)
+    bits = np.arange(1 << 16, dtype=np.uint32) << 16
+    v = bits.view(np.float32)
+    with np.errstate(invalid="ignore"):
+        v = np.where(np.abs(v) <= top, v, np.float32(0))
+    x = np.zeros((520, 128), dtype=np.float32)
+    x.reshape(-1)[:1 << 16] = v
+    x = np.concatenate([np.full((520, 1), top, dtype=np.float32), x[:, :127]], axis=1)
+    t = torch.from_numpy(x)
+    q = _poisoned(dr, 520, 128, 1)
+    dr.dr_quantize(t.cuda(), q[0])
+    torch.cuda.synchronize()
+    _check(*q, quant.quantize(x.astype(np.float64), 1))
+
+
+def test_empty_matrices_are_left_alone():
+    dr = _dr()
+    for rows, cols in ((0, 5), (5, 0), (0, 0)):
+        q, qt = dr.QMatrix.empty(rows, cols, 1), dr.QMatrix.empty(cols, rows, 1)
+        dr.dr_quantize(torch.empty((rows, cols), device="cuda"), q, qt)
+    torch.cuda.synchronize()

@@ -596,8 +596,8 @@ enum {
  *   c: device pointer, aligned to its type.
  *   workspace: device buffer (16-byte aligned) of at least the bytes that
  *   dr_qmatmul_workspace gives for these shapes; may be NULL where that is 0.
- * Errors: DR_EINVAL (limits above, K differs, row_stride < N, unknown flags, null
- * or misaligned pointers, workspace too small), DR_EHIP. */
+ * Errors: DR_EINVAL (limits above, M * N > 2^38, K differs, row_stride < N,
+ * unknown flags, null or misaligned pointers, workspace too small), DR_EHIP. */
 int dr_qmatmul(const dr_qmatrix* a, const dr_qmatrix* b, void* c, int32_t type, int64_t row_stride, int32_t flags,
                void* workspace, uint64_t workspace_bytes, void* stream);
 int dr_qmatmul_workspace(int64_t m, int64_t n, int64_t k, uint64_t* bytes);

@@ -18,14 +18,18 @@ struct ProductArgs {
   int64_t x_stride;
   void* c;
   int64_t c_stride;
-  uint32_t m, n, kb, tiles_n;
+  uint32_t m, n, kb, tiles_m, tiles_n;
   int32_t x_vec, c_vec, c_bf16, accumulate;
 };
+
+__device__ __forceinline__ i32x8 join(u32x4 lo, u32x4 hi) {
+  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
 
 // 32 codes of a row's 128-column block: p is the row at the block's first column plus 16 * lane group.
 __device__ __forceinline__ i32x8 load_codes(const uint8_t* p) {
   const u32x4 lo = *reinterpret_cast<const u32x4*>(p), hi = *reinterpret_cast<const u32x4*>(p + 64);
-  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  return join(lo, hi);
 }
 
 // The 128 columns' share of 16 x 16 outputs with exact products and sums: the values that 32 codes and their scale stand
@@ -179,6 +183,144 @@ void launch_direct(ProductArgs a, hipStream_t st) {
   hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), dim3(grid), dim3(64 * KS), 0, st, a);
 }
 
+// ------------------------------------------------------------------ large products
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 16 bytes per lane from memory to LDS, at `to` + 16 * lane; nothing passes through registers.
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+
+// Tile (tm, tn) of workgroup b: each XCD takes a contiguous eighth of the tiles, in bands of kBand tiles down, so that
+// the workgroups running at once on it share rows of both operands in its L2.
+constexpr uint32_t kBand = 8;
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+  const uint32_t t = xcd_tile(b, tiles_m * tiles_n);
+  const uint32_t band = t / (kBand * tiles_n), high = min(kBand, tiles_m - band * kBand), i = t - band * kBand * tiles_n;
+  tm = band * kBand + i % high;
+  tn = i / high;
+}
+
+// A tile of BM x BN of c per workgroup of WM * WN waves.  A step stages one 128-column block of BM rows of a and BN rows of
+// b in LDS (copied straight there, two buffers in turn), each row's eight 16-byte pieces at piece ^ row % 8, so that the
+// eight lanes which read the same piece of eight rows meet eight different bank groups.
+template <int BM, int BN, int WM, int WN, bool FAST>
+__global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs p) {
+  constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kRows = BM + BN, kCopies = kRows / 8 / kWaves;
+  static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && kRows % (8 * kWaves) == 0 && BM % (8 * kWaves) == 0, "tile");
+  __shared__ __align__(16) uint8_t lds[2][kRows * 128];
+  const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  uint32_t tm, tn;
+  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  const uint32_t m0 = tm * BM, n0 = tn * BN;
+  const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
+  const uint8_t* abase = p.a.data + (int64_t)m0 * p.a.stride;
+  const uint8_t* bbase = p.b.data + (int64_t)n0 * p.b.stride;
+
+  // copies: rows [0, BM) of the stage are a's, the others b's; rows past the matrix read its last one
+  uint32_t from[kCopies];
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) {
+    const uint32_t row = (i * kWaves + wave) * 8 + lane / 8, piece = (lane % 8) ^ (lane / 8);
+    if (i * kWaves * 8 < BM) from[i] = min(row, p.m - 1 - m0) * (uint32_t)p.a.stride + piece * 16;
+    else from[i] = min(row - BM, p.n - 1 - n0) * (uint32_t)p.b.stride + piece * 16;
+  }
+  auto stage = [&](uint32_t j, uint8_t* to) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      copy_to_lds((i * kWaves * 8 < BM ? abase : bbase) + (int64_t)j * 128 + from[i], to + (i * kWaves + wave) * 1024);
+  };
+
+  // scales: one word per row and four blocks
+  uint32_t ea[TM], eb[TN], next_a[TM], next_b[TN], arow[TM], brow[TN];
+#pragma unroll
+  for (int t = 0; t < TM; ++t) arow[t] = min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh;
+#pragma unroll
+  for (int t = 0; t < TN; ++t) brow[t] = min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh;
+  auto load_words = [&](uint32_t quad) {
+#pragma unroll
+    for (int t = 0; t < TM; ++t) next_a[t] = reinterpret_cast<const uint32_t*>(p.a.scales)[(int64_t)quad * p.a.srows + arow[t]];
+#pragma unroll
+    for (int t = 0; t < TN; ++t) next_b[t] = reinterpret_cast<const uint32_t*>(p.b.scales)[(int64_t)quad * p.b.srows + brow[t]];
+  };
+
+  // the lane's pieces: of each half h of the 128 columns, pieces 4h + 2g and 4h + 2g + 1
+  uint32_t at[2][2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) at[h][e] = r * 128 + (((h * 4 + g * 2 + e) ^ (r & 7)) * 16);
+
+  f32x16 acc[TN][TM] = {};
+  if (p.kb) {
+    load_words(0);
+    stage(0, lds[0]);
+  }
+  for (uint32_t j = 0; j < p.kb; ++j) {
+    // copies of block j have landed, and no wave reads the other buffer any more
+    __syncthreads();
+    if (j % 4 == 0) {
+#pragma unroll
+      for (int t = 0; t < TM; ++t) ea[t] = next_a[t];
+#pragma unroll
+      for (int t = 0; t < TN; ++t) eb[t] = next_b[t];
+    }
+    if (j + 1 < p.kb) {
+      stage(j + 1, lds[(j + 1) & 1]);
+      if (j % 4 == 3) load_words((j + 1) / 4);
+    }
+    const uint8_t* sa = lds[j & 1] + wm * 128;
+    const uint8_t* sb = lds[j & 1] + (BM + wn) * 128;
+    const uint32_t shift = j % 4 * 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i32x8 fa[TM], fb[TN];
+#pragma unroll
+      for (int t = 0; t < TN; ++t) fb[t] = join(*(const u32x4*)(sb + t * 4096 + at[h][0]), *(const u32x4*)(sb + t * 4096 + at[h][1]));
+#pragma unroll
+      for (int t = 0; t < TM; ++t) fa[t] = join(*(const u32x4*)(sa + t * 4096 + at[h][0]), *(const u32x4*)(sa + t * 4096 + at[h][1]));
+      if (FAST) {
+#pragma unroll
+        for (int x = 0; x < TN; ++x)
+#pragma unroll
+          for (int y = 0; y < TM; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[x], fa[y], acc[x][y], 0, 0, 0, (int)(eb[x] >> shift), 0, (int)(ea[y] >> shift));
+      } else {
+        Bf16Codes ca[TM];
+#pragma unroll
+        for (int y = 0; y < TM; ++y) ca[y] = to_bf16(fa[y], (int)(ea[y] >> shift & 255));
+#pragma unroll
+        for (int x = 0; x < TN; ++x) {
+          const Bf16Codes cb = to_bf16(fb[x], (int)(eb[x] >> shift & 255));
+#pragma unroll
+          for (int y = 0; y < TM; ++y)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb.v[i], ca[y].v[i], acc[x][y], 0, 0, 0);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < TN; ++x)
+#pragma unroll
+    for (int y = 0; y < TM; ++y)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store4(p, m0 + wm + y * 32 + r, n0 + wn + x * 32 + q * 8 + g * 4,
+               f32x4{acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]});
+}
+
+template <int BM, int BN, int WM, int WN>
+void launch_tile(ProductArgs a, bool fast, hipStream_t st) {
+  a.tiles_m = (uint32_t)ceil_div(a.m, BM);
+  a.tiles_n = (uint32_t)ceil_div(a.n, BN);
+  const dim3 grid(a.tiles_m * a.tiles_n), block(64 * WM * WN);
+  if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, false>), grid, block, 0, st, a);
+}
+
 }  // namespace
 
 hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
@@ -199,6 +341,8 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   if (l.x) {
     if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, st);
     else launch_direct<1, 1, 8, 1>(a, st);
+  } else if (l.m > 64) {
+    launch_tile<256, 256, 2, 4>(a, l.fast, st);
   } else {
     launch_direct<2, 4, 4, 0>(a, st);
   }

@@ -55,6 +55,11 @@ int check_dense(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t
   return DR_OK;
 }
 
+// The tiles of a launch are counted, and their lanes launched, in 32 bits.
+int check_results(int64_t m, int64_t n, const char* what) {
+  return m * n <= 1ll << 38 ? DR_OK : fail(DR_EINVAL, "%s: %lld x %lld results (at most 2^38)", what, (long long)m, (long long)n);
+}
+
 bool aligned_rows(const void* p, int64_t row_stride, int32_t type) {
   return aligned(p, 16) && row_stride * element_bytes(type) % 16 == 0;
 }
@@ -169,6 +174,7 @@ extern "C" int dr_qmatmul(const dr_qmatrix* a, const dr_qmatrix* b, void* c, int
   if (int rc = check_dense(c, type, a->rows, b->rows, row_stride, what, "c")) return rc;
   if (flags & ~(DR_ACCUMULATE | DR_FAST_SUMS)) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
   if ((flags & DR_ACCUMULATE) && type != DR_TYPE_F32) return fail(DR_EINVAL, "%s: DR_ACCUMULATE needs an fp32 c", what);
+  if (int rc = check_results(a->rows, b->rows, what)) return rc;
   uint64_t need = 0;
   if (int rc = dr_qmatmul_workspace(a->rows, b->rows, a->cols, &need)) return rc;
   if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
@@ -200,6 +206,7 @@ extern "C" int dr_qlinear(const void* x, int32_t x_type, int64_t m, int64_t x_ro
   if (int rc = check_dense(x, x_type, m, k, x_row_stride, what, "x")) return rc;
   if (int rc = check_dense(y, y_type, m, n, y_row_stride, what, "y")) return rc;
   if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
+  if (int rc = check_results(m, n, what)) return rc;
   const LinearSpace s = linear_space(m, n, k);
   if (int rc = check_workspace(workspace, workspace_bytes, s.total, what)) return rc;
   if (!m || !n) return DR_OK;

@@ -7,10 +7,14 @@
 // gives columns 16g.. and 64+16g.., so that each 16-byte load of a wave covers 64 consecutive bytes of 16 rows.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "quant_device.h"
 
 namespace dr {
 namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct ProductArgs {
   QView a, b;
@@ -73,6 +77,36 @@ __device__ __forceinline__ void store4(const ProductArgs& p, uint32_t m, uint32_
     }
   } else {
     float* c = static_cast<float*>(p.c) + at;
+    if (whole) {
+      f32x4* q = reinterpret_cast<f32x4*>(c);
+      *q = p.accumulate ? *q + v : v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n0 + i < p.n) c[i] = p.accumulate ? c[i] + v[i] : v[i];
+    }
+  }
+}
+
+// 16 bytes of results, columns n0 on, of row m of c.
+template <int BYTES>
+__device__ __forceinline__ void store_piece(const ProductArgs& p, uint32_t m, uint32_t n0, u32x4 w) {
+  constexpr int kElems = 16 / BYTES;
+  if (m >= p.m || n0 >= p.n) return;
+  const int64_t at = (int64_t)m * p.c_stride + n0;
+  const bool whole = p.c_vec && n0 + kElems <= p.n;
+  if (BYTES == 2) {
+    uint16_t* c = static_cast<uint16_t*>(p.c) + at;
+    if (whole) {
+      *reinterpret_cast<u32x4*>(c) = w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n0 + i < p.n) c[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+    }
+  } else {
+    float* c = static_cast<float*>(p.c) + at;
+    const f32x4 v = __builtin_bit_cast(f32x4, w);
     if (whole) {
       f32x4* q = reinterpret_cast<f32x4*>(c);
       *q = p.accumulate ? *q + v : v;
@@ -184,7 +218,6 @@ void launch_direct(ProductArgs a, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ large products
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // 16 bytes per lane from memory to LDS, at `to` + 16 * lane; nothing passes through registers.
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to) {
@@ -200,6 +233,40 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t t
   const uint32_t band = t / (kBand * tiles_n), high = min(kBand, tiles_m - band * kBand), i = t - band * kBand * tiles_n;
   tm = band * kBand + i % high;
   tn = i / high;
+}
+
+// Results of a wave, TM * 32 rows by TN * 32 columns from (m0, n0), through TM * TN * 2 KiB of LDS.
+template <int TM, int TN, int BYTES>
+__device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 (&acc)[TN][TM], uint8_t* lds, uint32_t m0, uint32_t n0, uint32_t lane) {
+  constexpr int kPitch = TN * 32 * BYTES, kPiecesRow = kPitch / 16, kPart = TM * 2 / BYTES;  // tiles down that fit at once
+  constexpr int kMask = kPiecesRow - 1, kRowsAt = 64 / kPiecesRow, kElems = 16 / BYTES;
+  static_assert(kPiecesRow <= 64 && (kPiecesRow & kMask) == 0, "rows of a power of two of pieces");
+  const uint32_t r = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int y0 = 0; y0 < TM; y0 += kPart) {
+#pragma unroll
+    for (int x = 0; x < TN; ++x)
+#pragma unroll
+      for (int y = 0; y < kPart; ++y)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x16& a = acc[x][y0 + y];
+          uint8_t* row = lds + (y * 32 + r) * kPitch;
+          const uint32_t col = x * 32 + q * 8 + g * 4;
+          if (BYTES == 2)
+            *reinterpret_cast<u32x2*>(row + (((col / 8) ^ (r & kMask)) * 16) + col % 8 * 2) = u32x2{bf16_pair(a[q * 4], a[q * 4 + 1]), bf16_pair(a[q * 4 + 2], a[q * 4 + 3])};
+          else
+            *reinterpret_cast<f32x4*>(row + (((col / 4) ^ (r & kMask)) * 16)) = f32x4{a[q * 4], a[q * 4 + 1], a[q * 4 + 2], a[q * 4 + 3]};
+        }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < kPart * 32 / kRowsAt; ++i) {
+      const uint32_t row = i * kRowsAt + lane / kPiecesRow, piece = lane % kPiecesRow;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + ((piece ^ (row & 31 & kMask)) * 16));
+      store_piece<BYTES>(p, m0 + y0 * 32 + row, n0 + piece * kElems, w);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // A tile of BM x BN of c per workgroup of WM * WN waves.  A step stages one 128-column block of BM rows of a and BN rows of
@@ -227,23 +294,27 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     if (i * kWaves * 8 < BM) from[i] = min(row, p.m - 1 - m0) * (uint32_t)p.a.stride + piece * 16;
     else from[i] = min(row - BM, p.n - 1 - n0) * (uint32_t)p.b.stride + piece * 16;
   }
-  auto stage = [&](uint32_t j, uint8_t* to) {
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i)
-      copy_to_lds((i * kWaves * 8 < BM ? abase : bbase) + (int64_t)j * 128 + from[i], to + (i * kWaves + wave) * 1024);
+  auto stage = [&](uint32_t j, uint8_t* to, int i) {
+    copy_to_lds((i * kWaves * 8 < BM ? abase : bbase) + (int64_t)j * 128 + from[i], to + (i * kWaves + wave) * 1024);
   };
 
-  // scales: one word per row and four blocks
-  uint32_t ea[TM], eb[TN], next_a[TM], next_b[TN], arow[TM], brow[TN];
+  // scale codes of one block column for the lane's rows
+  const uint8_t *acode[TM], *bcode[TN];
 #pragma unroll
-  for (int t = 0; t < TM; ++t) arow[t] = min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh;
+  for (int t = 0; t < TM; ++t) acode[t] = p.a.scales + 4 * (min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh);
 #pragma unroll
-  for (int t = 0; t < TN; ++t) brow[t] = min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh;
-  auto load_words = [&](uint32_t quad) {
+  for (int t = 0; t < TN; ++t) bcode[t] = p.b.scales + 4 * (min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh);
+  struct Scales {
+    int a[TM], b[TN];
+  };
+  auto load_scales = [&](uint32_t j) {
+    const int64_t at_a = (int64_t)(j / 4) * p.a.srows * 4 + j % 4, at_b = (int64_t)(j / 4) * p.b.srows * 4 + j % 4;
+    Scales s;
 #pragma unroll
-    for (int t = 0; t < TM; ++t) next_a[t] = reinterpret_cast<const uint32_t*>(p.a.scales)[(int64_t)quad * p.a.srows + arow[t]];
+    for (int t = 0; t < TM; ++t) s.a[t] = acode[t][at_a];
 #pragma unroll
-    for (int t = 0; t < TN; ++t) next_b[t] = reinterpret_cast<const uint32_t*>(p.b.scales)[(int64_t)quad * p.b.srows + brow[t]];
+    for (int t = 0; t < TN; ++t) s.b[t] = bcode[t][at_b];
+    return s;
   };
 
   // the lane's pieces: of each half h of the 128 columns, pieces 4h + 2g and 4h + 2g + 1
@@ -252,64 +323,92 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int e = 0; e < 2; ++e) at[h][e] = r * 128 + (((h * 4 + g * 2 + e) ^ (r & 7)) * 16);
+  // 16-byte pieces of one half block: two for each 32 rows, b's first
+  constexpr int kPieces = 2 * (TM + TN), kTiles = TM * TN;
+  struct Codes {
+    u32x4 piece[kPieces];
+  };
+  auto read_piece = [&](const uint8_t* from_lds, int h, int i) {
+    const int t = i / 2;
+    return *reinterpret_cast<const u32x4*>(from_lds + (t < TN ? (BM + wn) * 128 + t * 4096 : wm * 128 + (t - TN) * 4096) + at[h][i % 2]);
+  };
 
+  // One half block: its matrix instructions, and spread evenly among them what `between(i)` does for i of kTiles.
+  // Left alone the compiler would put all reads and copies behind them.
   f32x16 acc[TN][TM] = {};
-  if (p.kb) {
-    load_words(0);
-    stage(0, lds[0]);
-  }
-  for (uint32_t j = 0; j < p.kb; ++j) {
-    // copies of block j have landed, and no wave reads the other buffer any more
-    __syncthreads();
-    if (j % 4 == 0) {
+  auto multiply = [&](const Codes& c, const Scales& s, auto between) {
+    Bf16Codes ca[FAST ? 1 : TM], cb;
 #pragma unroll
-      for (int t = 0; t < TM; ++t) ea[t] = next_a[t];
+    for (int x = 0; x < TN; ++x)
 #pragma unroll
-      for (int t = 0; t < TN; ++t) eb[t] = next_b[t];
-    }
-    if (j + 1 < p.kb) {
-      stage(j + 1, lds[(j + 1) & 1]);
-      if (j % 4 == 3) load_words((j + 1) / 4);
-    }
-    const uint8_t* sa = lds[j & 1] + wm * 128;
-    const uint8_t* sb = lds[j & 1] + (BM + wn) * 128;
-    const uint32_t shift = j % 4 * 8;
+      for (int y = 0; y < TM; ++y) {
+        const i32x8 fb = join(c.piece[2 * x], c.piece[2 * x + 1]), fa = join(c.piece[2 * (TN + y)], c.piece[2 * (TN + y) + 1]);
+        between(x * TM + y);
+        if constexpr (FAST) {
+          acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb, fa, acc[x][y], 0, 0, 0, s.b[x], 0, s.a[y]);
+        } else {
+          if (x == 0) ca[y] = to_bf16(fa, s.a[y]);
+          if (y == 0) cb = to_bf16(fb, s.b[x]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i32x8 fa[TM], fb[TN];
-#pragma unroll
-      for (int t = 0; t < TN; ++t) fb[t] = join(*(const u32x4*)(sb + t * 4096 + at[h][0]), *(const u32x4*)(sb + t * 4096 + at[h][1]));
-#pragma unroll
-      for (int t = 0; t < TM; ++t) fa[t] = join(*(const u32x4*)(sa + t * 4096 + at[h][0]), *(const u32x4*)(sa + t * 4096 + at[h][1]));
-      if (FAST) {
-#pragma unroll
-        for (int x = 0; x < TN; ++x)
-#pragma unroll
-          for (int y = 0; y < TM; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[x], fa[y], acc[x][y], 0, 0, 0, (int)(eb[x] >> shift), 0, (int)(ea[y] >> shift));
-      } else {
-        Bf16Codes ca[TM];
-#pragma unroll
-        for (int y = 0; y < TM; ++y) ca[y] = to_bf16(fa[y], (int)(ea[y] >> shift & 255));
-#pragma unroll
-        for (int x = 0; x < TN; ++x) {
-          const Bf16Codes cb = to_bf16(fb[x], (int)(eb[x] >> shift & 255));
-#pragma unroll
-          for (int y = 0; y < TM; ++y)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb.v[i], ca[y].v[i], acc[x][y], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb.v[i], ca[y].v[i], acc[x][y], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0x6);  // vector and scalar arithmetic may move across
       }
+  };
+
+  // Step j: block j's second half is read while its first is multiplied; then, once every wave has read all of block
+  // j and block j + 1 has landed, block j + 2 starts on its way into block j's buffer and the first half of block j + 1
+  // is read while the second of block j is multiplied.
+  Codes first;
+  Scales now, next;
+  auto step = [&](uint32_t j, auto more, auto last) {
+    uint8_t *cur = lds[j & 1], *other = lds[(j + 1) & 1];
+    Codes second;
+    multiply(first, now, [&](int i) {
+#pragma unroll
+      for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) second.piece[k] = read_piece(cur, 1, k);
+    });
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    const Scales landed = next;
+    if constexpr (decltype(more)::value) next = load_scales(j + 2);
+    multiply(second, now, [&](int i) {
+      if constexpr (!decltype(last)::value) {
+#pragma unroll
+        for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) first.piece[k] = read_piece(other, 0, k);
+      }
+      if constexpr (decltype(more)::value) {
+#pragma unroll
+        for (int k = i * kCopies / kTiles; k < (i + 1) * kCopies / kTiles; ++k) stage(j + 2, cur, k);
+      }
+    });
+    now = landed;
+  };
+  if (p.kb) {
+    const uint32_t kb = p.kb;
+    now = load_scales(0);
+    next = load_scales(min(1u, kb - 1));
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) stage(0, lds[0], i);
+    __syncthreads();
+    if (kb > 1) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) stage(1, lds[1], i);
     }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds[0], 0, i);
+    for (uint32_t j = 0; j + 2 < kb; ++j) step(j, std::true_type{}, std::false_type{});
+    if (kb > 1) step(kb - 2, std::false_type{}, std::false_type{});
+    step(kb - 1, std::false_type{}, std::true_type{});
   }
-#pragma unroll
-  for (int x = 0; x < TN; ++x)
-#pragma unroll
-    for (int y = 0; y < TM; ++y)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store4(p, m0 + wm + y * 32 + r, n0 + wn + x * 32 + q * 8 + g * 4,
-               f32x4{acc[x][y][q * 4], acc[x][y][q * 4 + 1], acc[x][y][q * 4 + 2], acc[x][y][q * 4 + 3]});
+  // Each wave turns its results in its own part of the LDS, so that they leave as whole rows of TN * 32 columns: 16-byte
+  // pieces, at piece ^ row % 32 of a row.
+  __syncthreads();
+  constexpr int kOut = BM * BN / kWaves;  // results of a wave
+  uint8_t* mine = lds[0] + wave * (sizeof(lds) / kWaves);
+  if (p.c_bf16) store_turned<TM, TN, 2>(p, acc, mine, m0 + wm, n0 + wn, lane);
+  else store_turned<TM, TN, 4>(p, acc, mine, m0 + wm, n0 + wn, lane);
+  static_assert(kOut * 2 <= (int)sizeof(lds) / kWaves, "a wave's bf16 results fit its part");
 }
 
 template <int BM, int BN, int WM, int WN>
@@ -335,14 +434,14 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   a.n = l.n;
   a.kb = l.kb;
   a.x_vec = l.x_aligned;
-  a.c_vec = reinterpret_cast<uintptr_t>(l.c) % (l.c_bf16 ? 8 : 16) == 0 && l.c_stride % 4 == 0;
+  a.c_vec = reinterpret_cast<uintptr_t>(l.c) % 16 == 0 && l.c_stride * (l.c_bf16 ? 2 : 4) % 16 == 0;
   a.c_bf16 = l.c_bf16;
   a.accumulate = l.accumulate;
   if (l.x) {
     if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, st);
     else launch_direct<1, 1, 8, 1>(a, st);
   } else if (l.m > 64) {
-    launch_tile<256, 256, 2, 4>(a, l.fast, st);
+    launch_tile<256, 256, 2, 2>(a, l.fast, st);
   } else {
     launch_direct<2, 4, 4, 0>(a, st);
   }

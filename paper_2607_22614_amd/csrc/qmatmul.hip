@@ -219,10 +219,14 @@ void launch_direct(ProductArgs a, hipStream_t st) {
 
 // ------------------------------------------------------------------ large products
 
-// 16 bytes per lane from memory to LDS, at `to` + 16 * lane; nothing passes through registers.
-__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint8_t* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
-                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+// 16 bytes per lane from memory to LDS, at `to` + 16 * lane; nothing passes through registers.  As a buffer access its
+// address is the tile's base, the lane's offset and the step's, with no arithmetic in between.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_at(const uint8_t* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, 0xFFFFFFFFu, 0x00027000);  // raw, 32-bit data
+}
+__device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lane_at, uint32_t at, uint8_t* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)lane_at, (int)at, 0, 0);
 }
 
 // Tile (tm, tn) of workgroup b: each XCD takes a contiguous eighth of the tiles, in bands of kBand tiles down, so that
@@ -270,8 +274,8 @@ __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 
 }
 
 // A tile of BM x BN of c per workgroup of WM * WN waves.  A step stages one 128-column block of BM rows of a and BN rows of
-// b in LDS (copied straight there, two buffers in turn), each row's eight 16-byte pieces at piece ^ row % 8, so that the
-// eight lanes which read the same piece of eight rows meet eight different bank groups.
+// b in LDS (copied straight there, two buffers in turn), each row's eight 16-byte pieces at piece ^ row / 2 % 8: the
+// sixteen lanes that read at once, the same piece of sixteen rows, then meet all 64 banks.
 template <int BM, int BN, int WM, int WN, bool FAST>
 __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs p) {
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kRows = BM + BN, kCopies = kRows / 8 / kWaves;
@@ -283,37 +287,37 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
   const uint32_t m0 = tm * BM, n0 = tn * BN;
   const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
-  const uint8_t* abase = p.a.data + (int64_t)m0 * p.a.stride;
-  const uint8_t* bbase = p.b.data + (int64_t)n0 * p.b.stride;
+  const Buffer abase = buffer_at(p.a.data + (int64_t)m0 * p.a.stride);
+  const Buffer bbase = buffer_at(p.b.data + (int64_t)n0 * p.b.stride);
 
   // copies: rows [0, BM) of the stage are a's, the others b's; rows past the matrix read its last one
   uint32_t from[kCopies];
 #pragma unroll
   for (int i = 0; i < kCopies; ++i) {
-    const uint32_t row = (i * kWaves + wave) * 8 + lane / 8, piece = (lane % 8) ^ (lane / 8);
+    const uint32_t row = (i * kWaves + wave) * 8 + lane / 8, piece = (lane % 8) ^ (row / 2 % 8);
     if (i * kWaves * 8 < BM) from[i] = min(row, p.m - 1 - m0) * (uint32_t)p.a.stride + piece * 16;
     else from[i] = min(row - BM, p.n - 1 - n0) * (uint32_t)p.b.stride + piece * 16;
   }
   auto stage = [&](uint32_t j, uint8_t* to, int i) {
-    copy_to_lds((i * kWaves * 8 < BM ? abase : bbase) + (int64_t)j * 128 + from[i], to + (i * kWaves + wave) * 1024);
+    copy_to_lds(i * kWaves * 8 < BM ? abase : bbase, from[i], j * 128, to + (i * kWaves + wave) * 1024);
   };
 
-  // scale codes of one block column for the lane's rows
-  const uint8_t *acode[TM], *bcode[TN];
+  // scale codes of one block column for the lane's rows (a matrix's scales are a 128th of its data: below 2^32 bytes)
+  const Buffer ascales = buffer_at(p.a.scales), bscales = buffer_at(p.b.scales);
+  uint32_t acode[TM], bcode[TN];
 #pragma unroll
-  for (int t = 0; t < TM; ++t) acode[t] = p.a.scales + 4 * (min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh);
+  for (int t = 0; t < TM; ++t) acode[t] = 4 * (min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh);
 #pragma unroll
-  for (int t = 0; t < TN; ++t) bcode[t] = p.b.scales + 4 * (min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh);
+  for (int t = 0; t < TN; ++t) bcode[t] = 4 * (min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh);
   struct Scales {
     int a[TM], b[TN];
   };
   auto load_scales = [&](uint32_t j) {
-    const int64_t at_a = (int64_t)(j / 4) * p.a.srows * 4 + j % 4, at_b = (int64_t)(j / 4) * p.b.srows * 4 + j % 4;
     Scales s;
 #pragma unroll
-    for (int t = 0; t < TM; ++t) s.a[t] = acode[t][at_a];
+    for (int t = 0; t < TM; ++t) s.a[t] = __builtin_amdgcn_raw_buffer_load_b8(ascales, (int)acode[t], (int)(j / 4 * p.a.srows * 4 + j % 4), 0);
 #pragma unroll
-    for (int t = 0; t < TN; ++t) s.b[t] = bcode[t][at_b];
+    for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)bcode[t], (int)(j / 4 * p.b.srows * 4 + j % 4), 0);
     return s;
   };
 
@@ -322,7 +326,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) at[h][e] = r * 128 + (((h * 4 + g * 2 + e) ^ (r & 7)) * 16);
+    for (int e = 0; e < 2; ++e) at[h][e] = r * 128 + (((h * 4 + g * 2 + e) ^ (r / 2 % 8)) * 16);
   // 16-byte pieces of one half block: two for each 32 rows, b's first
   constexpr int kPieces = 2 * (TM + TN), kTiles = TM * TN;
   struct Codes {
@@ -370,6 +374,11 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     });
     __syncthreads();
     __builtin_amdgcn_sched_barrier(0);
+    // used from here on only: copied any earlier, they would be waited for there, and all copies with them
+#pragma unroll
+    for (int t = 0; t < TM; ++t) asm volatile("" : "+v"(next.a[t]));
+#pragma unroll
+    for (int t = 0; t < TN; ++t) asm volatile("" : "+v"(next.b[t]));
     const Scales landed = next;
     if constexpr (decltype(more)::value) next = load_scales(j + 2);
     multiply(second, now, [&](int i) {

@@ -74,6 +74,56 @@ def test_product(m, n, k, blocks):
     _close(out, want + s, size + np.abs(s), k, False)
 
 
+def _groups(a, b):
+    """sum over groups of 8 adjacent columns of the largest |a||b| of the group."""
+    k = -a.shape[1] % 8
+    a, b = (np.abs(np.pad(v, ((0, 0), (0, k)))).reshape(v.shape[0], -1, 8) for v in (a, b))
+    return sum((a[:, None, g] * b[None, :, g]).max(axis=2) for g in range(a.shape[1]))
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("blocks", [(1, 128), (1, 1), (128, 128)])
+def test_fast_sums(m, n, k, blocks):
+    """Each product of 8 adjacent columns may lose what lies below 2^-13 of the largest one's power of two, so at most
+    2^-13 of the largest product: 8 * 2^-13 of it per group, beside the tolerance of the exact sums."""
+    dr = _dr()
+    a, av = _matrix(dr, m, k, blocks[0], m + k, extra=16)
+    b, bv = _matrix(dr, n, k, blocks[1], n + k + 1, extra=48)
+    want, size = quant.product(av, bv)
+    tol = 2.0**-10 * _groups(av, bv) + (-(-k // 128) * 128 + 64) * 2.0**-23 * size
+    ws = _workspace(dr, m, n, k)
+    start = torch.from_numpy(np.random.default_rng(5).standard_normal((m, n)).astype(np.float32) * float(np.abs(want).mean() + 1))
+    for dtype, accumulate in ((torch.float32, False), (torch.bfloat16, False), (torch.float32, True)):
+        say("fast", m, n, k, blocks, dtype, accumulate)
+        out = torch.full((m + 1, n), 7.0, dtype=dtype, device="cuda")
+        add = start.to(torch.float64).numpy() if accumulate else 0.0
+        if accumulate:
+            out[:m] = start.cuda()
+        dr.dr_qmatmul(a, b, out[:m], accumulate=accumulate, fast=True, workspace=ws)
+        torch.cuda.synchronize()
+        got = out[:m].to(torch.float64).cpu().numpy()
+        bound = tol + (np.abs(want) * 2.0**-8 if dtype == torch.bfloat16 else 2.0**-22 * np.abs(add))
+        assert (np.abs(got - want - add) <= bound).all()
+        assert (out[m] == 7.0).all()
+
+
+def test_fast_sums_of_normal_values():
+    """Normally distributed values: a group's 8 products lose less than 2^-13 of its largest each, with signs of their own,
+    so of the norm at most sqrt(8 * 2^-26 * E[largest^2] / (8 * E[product^2])) <= 2^-13 * sqrt(8)."""
+    dr = _dr()
+    say("fast, normal values")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, w = torch.randn((300, 4096), generator=gen, device="cuda"), torch.randn((520, 4096), generator=gen, device="cuda")
+    a, b = dr.QMatrix.empty(300, 4096, 1), dr.QMatrix.empty(520, 4096, 128)
+    dr.dr_quantize(x, a), dr.dr_quantize(w, b)
+    out = torch.empty((300, 520), device="cuda")
+    dr.dr_qmatmul(a, b, out, fast=True, workspace=_workspace(dr, 300, 520, 4096))
+    av = quant.values(a.data.cpu().numpy(), a.scales.cpu().numpy(), 4096, 1)
+    bv = quant.values(b.data.cpu().numpy(), b.scales.cpu().numpy(), 4096, 128)
+    want = av @ bv.T
+    assert np.linalg.norm(out.cpu().numpy() - want) <= 2.0**-13 * np.sqrt(8) * np.linalg.norm(want)
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 50, 300), (130, 150, 300), (300, 290, 150)])
 @pytest.mark.parametrize("offset,stride", [(1, 1), (4, 8), (2, 0)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])

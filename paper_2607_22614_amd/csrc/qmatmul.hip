@@ -7,6 +7,7 @@
 // gives columns 16g.. and 64+16g.., so that each 16-byte load of a wave covers 64 consecutive bytes of 16 rows.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "quant_device.h"
@@ -23,7 +24,10 @@ struct ProductArgs {
   void* c;
   int64_t c_stride;
   uint32_t m, n, kb, tiles_m, tiles_n;
+  uint32_t splits;  // of the blocks: workgroups of one tile, whose fp32 sums go to part[split][m][part_stride]
   int32_t x_vec, c_vec, c_bf16, accumulate;
+  float* part;
+  int64_t part_stride;
 };
 
 __device__ __forceinline__ i32x8 join(u32x4 lo, u32x4 hi) {
@@ -54,12 +58,6 @@ __device__ __forceinline__ Bf16Codes to_bf16(i32x8 codes, int code) {
     }
   return r;
 }
-__device__ __forceinline__ f32x4 mfma(const Bf16Codes& a, const Bf16Codes& b, f32x4 c) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], c, 0, 0, 0);
-  return c;
-}
-
 // Columns n0 .. n0+3 of row m of c.
 __device__ __forceinline__ void store4(const ProductArgs& p, uint32_t m, uint32_t n0, f32x4 v) {
   if (m >= p.m || n0 >= p.n) return;
@@ -118,24 +116,61 @@ __device__ __forceinline__ void store_piece(const ProductArgs& p, uint32_t m, ui
   }
 }
 
-// Codes and scale of 128 columns of one row of x, quantized as dr_quantize does; each lane holds 32 of them.
-template <bool BF16>
-__device__ __forceinline__ i32x8 quantize_block(const ProductArgs& p, uint32_t row, uint32_t col, int& code) {
-  float v[4][8];
+// A lane's 32 elements of 128 columns of one row of x (X: 1 fp32, 2 bf16), as they lie in memory.
+template <int X>
+struct Elements {
+  u32x4 w[X == 0 ? 1 : X == 1 ? 8 : 4];
+};
+template <int X>
+__device__ __forceinline__ Elements<X> load_elements(const ProductArgs& p, uint32_t row, uint32_t col) {
+  Elements<X> e;
+  const int64_t at = (int64_t)row * p.x_stride;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t c = col + (q >> 1) * 64 + (q & 1) * 8;
-    load8<BF16>(p.x, (int64_t)row * p.x_stride + c, max(0, min(8, (int)p.a.cols - (int)c)), p.x_vec, v[q]);
+    const int n = max(0, min(8, (int)p.a.cols - (int)c));
+    if constexpr (X == 2) {
+      const uint16_t* x = static_cast<const uint16_t*>(p.x) + at + c;
+      if (p.x_vec && n == 8) {
+        e.w[q] = *reinterpret_cast<const u32x4*>(x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.w[q][i] = (2 * i < n ? x[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)x[2 * i + 1] << 16 : 0u);
+      }
+    } else {
+      const uint32_t* x = static_cast<const uint32_t*>(p.x) + at + c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (p.x_vec && n == 8) {
+          e.w[2 * q + h] = *reinterpret_cast<const u32x4*>(x + 4 * h);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e.w[2 * q + h][i] = 4 * h + i < n ? x[4 * h + i] : 0u;
+        }
+      }
+    }
   }
+  return e;
+}
+template <int X>
+__device__ __forceinline__ float element(const Elements<X>& e, int i) {
+  if constexpr (X == 1) return __uint_as_float(e.w[i / 4][i % 4]);
+  const uint32_t w = e.w[i / 8][i % 8 / 2];
+  return __uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16);
+}
+
+// Their codes, and the scale of the row's 128 columns, as dr_quantize gives them.
+template <int X>
+__device__ __forceinline__ i32x8 quantize_block(const Elements<X>& e, int& code) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) m = max(m, abs_bits(v[i / 8][i % 8]));
+  for (int i = 0; i < 32; ++i) m = max(m, abs_bits(element(e, i)));
   m = max_rows(m);
   const bool odd = __any(m >= kInfBits);
   if (odd) {
     m = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m = max(m, finite_bits(v[i / 8][i % 8]));
+    for (int i = 0; i < 32; ++i) m = max(m, finite_bits(element(e, i)));
     m = max_rows(m);
   }
   code = (int)scale_code(m);
@@ -143,59 +178,91 @@ __device__ __forceinline__ i32x8 quantize_block(const ProductArgs& p, uint32_t r
   i32x8 w;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float* f = &v[i / 2][(i % 2) * 4];
-    w[i] = (int)(odd ? to_e4m3<true>(f[0], f[1], f[2], f[3], inv) : to_e4m3<false>(f[0], f[1], f[2], f[3], inv));
+    const float f0 = element(e, 4 * i), f1 = element(e, 4 * i + 1), f2 = element(e, 4 * i + 2), f3 = element(e, 4 * i + 3);
+    w[i] = (int)(odd ? to_e4m3<true>(f0, f1, f2, f3, inv) : to_e4m3<false>(f0, f1, f2, f3, inv));
   }
   return w;
 }
 
-// Scale code of block column j for the lane's block row.
-__device__ __forceinline__ int load_code(const QView& q, uint32_t row, uint32_t j) {
-  return q.scales[((int64_t)(j >> 2) * q.srows + (row >> q.sh)) * 4 + (j & 3)];
-}
-
-// A tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
-// instructions; the KS waves of the workgroup take the 128-column blocks in turn and join their sums in LDS, in the
-// order of the waves.  X: 0 takes a from its codes, 1 quantizes fp32 rows of x, 2 bf16 rows.
-template <int FT, int TT, int KS, int X>
+// Few rows: a tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
+// instructions; the KS waves of the workgroup take the 128-column blocks in turn, each loading its next block while it
+// multiplies one, and join their sums in LDS, in the order of the waves.  X: 0 takes a from its codes, 1 quantizes fp32
+// rows of x, 2 bf16 rows.
+template <int FT, int TT, int KS, int X, bool FAST>
 __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) {
   __shared__ f32x4 part[KS][FT * TT][64];
   const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t n0 = blockIdx.x % p.tiles_n * (FT * 16), m0 = blockIdx.x / p.tiles_n * (TT * 16);
-  const uint8_t *bp[FT], *ap[TT];
-  uint32_t brow[FT], arow[TT];
+  const uint8_t *bp[FT], *ap[TT], *bcode[FT], *acode[TT];
+  uint32_t arow[TT];
 #pragma unroll
   for (int f = 0; f < FT; ++f) {
-    brow[f] = min(n0 + f * 16 + r, p.n - 1);
-    bp[f] = p.b.data + (int64_t)brow[f] * p.b.stride + g * 16;
+    const uint32_t row = min(n0 + f * 16 + r, p.n - 1);
+    bp[f] = p.b.data + (int64_t)row * p.b.stride + g * 16;
+    bcode[f] = p.b.scales + 4 * (row >> p.b.sh);
   }
 #pragma unroll
   for (int t = 0; t < TT; ++t) {
     arow[t] = min(m0 + t * 16 + r, p.m - 1);
     ap[t] = p.a.data + (int64_t)arow[t] * p.a.stride + g * 16;
+    acode[t] = p.a.scales + 4 * (arow[t] >> p.a.sh);
   }
-  f32x4 acc[FT][TT] = {};
-  for (uint32_t j = wave; j < p.kb; j += KS) {
-    Bf16Codes bw[FT], aw[TT];
+  struct Block {
+    i32x8 b[FT], a[X ? 1 : TT];
+    int eb[FT], ea[TT];
+    Elements<X> x[X ? TT : 1];
+  };
+  auto load = [&](uint32_t j) {
+    Block k;
 #pragma unroll
     for (int f = 0; f < FT; ++f) {
-      bw[f] = to_bf16(load_codes(bp[f] + (int64_t)j * 128), load_code(p.b, brow[f], j));
+      k.b[f] = load_codes(bp[f] + (int64_t)j * 128);
+      k.eb[f] = bcode[f][(int64_t)(j >> 2) * p.b.srows * 4 + (j & 3)];
     }
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-      if (X == 0) {
-        aw[t] = to_bf16(load_codes(ap[t] + (int64_t)j * 128), load_code(p.a, arow[t], j));
+      if constexpr (X != 0) {
+        k.x[t] = load_elements<X>(p, arow[t], j * 128 + g * 16);
       } else {
-        int code;
-        const i32x8 w = quantize_block<X == 2>(p, arow[t], j * 128 + g * 16, code);
-        aw[t] = to_bf16(w, code);
+        k.a[t] = load_codes(ap[t] + (int64_t)j * 128);
+        k.ea[t] = acode[t][(int64_t)(j >> 2) * p.a.srows * 4 + (j & 3)];
       }
     }
+    return k;
+  };
+  f32x4 acc[FT][TT] = {};
+  if (wave < p.kb) {
+    Block next = load(wave);
+    for (uint32_t j = wave; j < p.kb; j += KS) {
+      Block k = next;
+      next = load(min(j + KS, p.kb - 1));
+      i32x8 aw[TT];
 #pragma unroll
-    for (int f = 0; f < FT; ++f)
+      for (int t = 0; t < TT; ++t) {
+        if constexpr (X != 0) aw[t] = quantize_block(k.x[t], k.ea[t]);
+        else aw[t] = k.a[t];
+      }
+      if constexpr (FAST) {
 #pragma unroll
-      for (int t = 0; t < TT; ++t) acc[f][t] = mfma(bw[f], aw[t], acc[f][t]);
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+          for (int t = 0; t < TT; ++t)
+            acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.b[f], aw[t], acc[f][t], 0, 0, 0, k.eb[f], 0, k.ea[t]);
+      } else {
+        Bf16Codes ca[TT];
+#pragma unroll
+        for (int t = 0; t < TT; ++t) ca[t] = to_bf16(aw[t], k.ea[t]);
+#pragma unroll
+        for (int f = 0; f < FT; ++f) {
+          const Bf16Codes cb = to_bf16(k.b[f], k.eb[f]);
+#pragma unroll
+          for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.v[i], ca[t].v[i], acc[f][t], 0, 0, 0);
+        }
+      }
+    }
   }
 #pragma unroll
   for (int f = 0; f < FT; ++f)
@@ -211,10 +278,11 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
 }
 
 template <int FT, int TT, int KS, int X>
-void launch_direct(ProductArgs a, hipStream_t st) {
+void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
   a.tiles_n = (uint32_t)ceil_div(a.n, FT * 16);
-  const uint32_t grid = a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16);
-  hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), dim3(grid), dim3(64 * KS), 0, st, a);
+  const dim3 grid(a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16)), block(64 * KS);
+  if (fast) hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, false>), grid, block, 0, st, a);
 }
 
 // ------------------------------------------------------------------ large products
@@ -232,11 +300,13 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lane_at, uint3
 // Tile (tm, tn) of workgroup b: each XCD takes a contiguous eighth of the tiles, in bands of kBand tiles down, so that
 // the workgroups running at once on it share rows of both operands in its L2.
 constexpr uint32_t kBand = 8;
-__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
-  const uint32_t t = xcd_tile(b, tiles_m * tiles_n);
+// Returns the split: whole products of tiles follow one another.
+__device__ __forceinline__ uint32_t tile_of(uint32_t b, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits, uint32_t& tm, uint32_t& tn) {
+  const uint32_t all = xcd_tile(b, tiles_m * tiles_n * splits), split = all / (tiles_m * tiles_n), t = all % (tiles_m * tiles_n);
   const uint32_t band = t / (kBand * tiles_n), high = min(kBand, tiles_m - band * kBand), i = t - band * kBand * tiles_n;
   tm = band * kBand + i % high;
   tn = i / high;
+  return split;
 }
 
 // Results of a wave, TM * 32 rows by TN * 32 columns from (m0, n0), through TM * TN * 2 KiB of LDS.
@@ -284,7 +354,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   uint32_t tm, tn;
-  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  const uint32_t split = tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn);
   const uint32_t m0 = tm * BM, n0 = tn * BN;
   const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
   const Buffer abase = buffer_at(p.a.data + (int64_t)m0 * p.a.stride);
@@ -393,40 +463,61 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     });
     now = landed;
   };
-  if (p.kb) {
-    const uint32_t kb = p.kb;
-    now = load_scales(0);
-    next = load_scales(min(1u, kb - 1));
+  const uint32_t j0 = (uint32_t)((uint64_t)p.kb * split / p.splits), j1 = (uint32_t)((uint64_t)p.kb * (split + 1) / p.splits);
+  if (j0 < j1) {
+    now = load_scales(j0);
+    next = load_scales(min(j0 + 1, j1 - 1));
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) stage(0, lds[0], i);
+    for (int i = 0; i < kCopies; ++i) stage(j0, lds[j0 & 1], i);
     __syncthreads();
-    if (kb > 1) {
+    if (j0 + 1 < j1) {
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) stage(1, lds[1], i);
+      for (int i = 0; i < kCopies; ++i) stage(j0 + 1, lds[(j0 + 1) & 1], i);
     }
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds[0], 0, i);
-    for (uint32_t j = 0; j + 2 < kb; ++j) step(j, std::true_type{}, std::false_type{});
-    if (kb > 1) step(kb - 2, std::false_type{}, std::false_type{});
-    step(kb - 1, std::false_type{}, std::true_type{});
+    for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds[j0 & 1], 0, i);
+    for (uint32_t j = j0; j + 2 < j1; ++j) step(j, std::true_type{}, std::false_type{});
+    if (j0 + 1 < j1) step(j1 - 2, std::false_type{}, std::false_type{});
+    step(j1 - 1, std::false_type{}, std::true_type{});
   }
   // Each wave turns its results in its own part of the LDS, so that they leave as whole rows of TN * 32 columns: 16-byte
   // pieces, at piece ^ row % 32 of a row.
   __syncthreads();
   constexpr int kOut = BM * BN / kWaves;  // results of a wave
   uint8_t* mine = lds[0] + wave * (sizeof(lds) / kWaves);
+  if (p.splits > 1) {
+    p.c = p.part + (int64_t)split * p.m * p.part_stride;
+    p.c_stride = p.part_stride;
+    p.c_vec = 1;
+    p.c_bf16 = p.accumulate = 0;
+  }
   if (p.c_bf16) store_turned<TM, TN, 2>(p, acc, mine, m0 + wm, n0 + wn, lane);
   else store_turned<TM, TN, 4>(p, acc, mine, m0 + wm, n0 + wn, lane);
   static_assert(kOut * 2 <= (int)sizeof(lds) / kWaves, "a wave's bf16 results fit its part");
+}
+
+// c from the sums of the splits, in their order; a lane takes four columns.
+__global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs p) {
+  const uint32_t groups = (uint32_t)(p.part_stride / 4);
+  const uint64_t n = (uint64_t)p.m * groups;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+    const uint32_t m = (uint32_t)(i / groups), n0 = (uint32_t)(i % groups) * 4;
+    const float* part = p.part + (int64_t)m * p.part_stride + n0;
+    f32x4 s = *reinterpret_cast<const f32x4*>(part);
+    for (uint32_t k = 1; k < p.splits; ++k) s += *reinterpret_cast<const f32x4*>(part + (int64_t)k * p.m * p.part_stride);
+    store4(p, m, n0, s);
+  }
 }
 
 template <int BM, int BN, int WM, int WN>
 void launch_tile(ProductArgs a, bool fast, hipStream_t st) {
   a.tiles_m = (uint32_t)ceil_div(a.m, BM);
   a.tiles_n = (uint32_t)ceil_div(a.n, BN);
-  const dim3 grid(a.tiles_m * a.tiles_n), block(64 * WM * WN);
+  const dim3 grid(a.tiles_m * a.tiles_n * a.splits), block(64 * WM * WN);
   if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, false>), grid, block, 0, st, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL(join_splits_kernel, dim3((uint32_t)std::min<int64_t>(2048, ceil_div(a.m * (a.part_stride / 4), 256))), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -447,12 +538,19 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   a.c_bf16 = l.c_bf16;
   a.accumulate = l.accumulate;
   if (l.x) {
-    if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, st);
-    else launch_direct<1, 1, 8, 1>(a, st);
-  } else if (l.m > 64) {
-    launch_tile<256, 256, 2, 2>(a, l.fast, st);
+    if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, l.fast, st);
+    else launch_direct<1, 1, 8, 1>(a, l.fast, st);
+  } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect) {
+    a.splits = plan.splits;
+    a.part = static_cast<float*>(l.workspace);
+    a.part_stride = part_stride(l.n);
+    if (plan.kind == ProductPlan::kTile256) launch_tile<256, 256, 2, 2>(a, l.fast, st);
+    else launch_tile<128, 128, 2, 2>(a, l.fast, st);
   } else {
-    launch_direct<2, 4, 4, 0>(a, st);
+    if (l.m <= 16) launch_direct<2, 1, 8, 0>(a, l.fast, st);
+    else if (l.m <= 32) launch_direct<2, 2, 8, 0>(a, l.fast, st);
+    else if (l.m <= 48) launch_direct<2, 3, 8, 0>(a, l.fast, st);
+    else launch_direct<2, 4, 8, 0>(a, l.fast, st);
   }
   return hipGetLastError();
 }

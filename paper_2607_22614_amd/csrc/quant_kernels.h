@@ -51,4 +51,14 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st);
 // Rows that launch_product quantizes itself.
 constexpr uint32_t kFusedRows = 16;
 
+// How a product of 8-bit operands is cut: tiles of one of two sizes, and each tile's blocks over `splits` workgroups
+// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows.
+struct ProductPlan {
+  enum Kind { kDirect, kTile128, kTile256 } kind;
+  uint32_t splits;
+};
+inline int64_t part_stride(int64_t n) { return ceil_div(n, 4) * 4; }
+
+ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast);
+
 }  // namespace dr

@@ -119,44 +119,17 @@ __device__ __forceinline__ void store_piece(const ProductArgs& p, uint32_t m, ui
 // A lane's 32 elements of 128 columns of one row of x (X: 1 fp32, 2 bf16), as they lie in memory.
 template <int X>
 struct Elements {
-  u32x4 w[X == 0 ? 1 : X == 1 ? 8 : 4];
+  Raw8<X == 2> v[X == 0 ? 1 : 4];
 };
 template <int X>
 __device__ __forceinline__ Elements<X> load_elements(const ProductArgs& p, uint32_t row, uint32_t col) {
   Elements<X> e;
-  const int64_t at = (int64_t)row * p.x_stride;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t c = col + (q >> 1) * 64 + (q & 1) * 8;
-    const int n = max(0, min(8, (int)p.a.cols - (int)c));
-    if constexpr (X == 2) {
-      const uint16_t* x = static_cast<const uint16_t*>(p.x) + at + c;
-      if (p.x_vec && n == 8) {
-        e.w[q] = *reinterpret_cast<const u32x4*>(x);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e.w[q][i] = (2 * i < n ? x[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)x[2 * i + 1] << 16 : 0u);
-      }
-    } else {
-      const uint32_t* x = static_cast<const uint32_t*>(p.x) + at + c;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (p.x_vec && n == 8) {
-          e.w[2 * q + h] = *reinterpret_cast<const u32x4*>(x + 4 * h);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e.w[2 * q + h][i] = 4 * h + i < n ? x[4 * h + i] : 0u;
-        }
-      }
-    }
+    e.v[q] = load_raw8<X == 2>(p.x, (int64_t)row * p.x_stride + c, max(0, min(8, (int)p.a.cols - (int)c)), p.x_vec);
   }
   return e;
-}
-template <int X>
-__device__ __forceinline__ float element(const Elements<X>& e, int i) {
-  if constexpr (X == 1) return __uint_as_float(e.w[i / 4][i % 4]);
-  const uint32_t w = e.w[i / 8][i % 8 / 2];
-  return __uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16);
 }
 
 // Their codes, and the scale of the row's 128 columns, as dr_quantize gives them.
@@ -164,22 +137,19 @@ template <int X>
 __device__ __forceinline__ i32x8 quantize_block(const Elements<X>& e, int& code) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) m = max(m, abs_bits(element(e, i)));
-  m = max_rows(m);
-  const bool odd = __any(m >= kInfBits);
-  if (odd) {
+  for (int q = 0; q < 4; ++q) m = max(m, row_max(e.v[q], false));
+  if (__any(m >= kInfBits)) {
     m = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m = max(m, finite_bits(element(e, i)));
-    m = max_rows(m);
+    for (int q = 0; q < 4; ++q) m = max(m, row_max(e.v[q], true));
   }
-  code = (int)scale_code(m);
-  const float inv = inverse_scale((uint32_t)code);
+  code = (int)scale_code(max_rows(m));
   i32x8 w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float f0 = element(e, 4 * i), f1 = element(e, 4 * i + 1), f2 = element(e, 4 * i + 2), f3 = element(e, 4 * i + 3);
-    w[i] = (int)(odd ? to_e4m3<true>(f0, f1, f2, f3, inv) : to_e4m3<false>(f0, f1, f2, f3, inv));
+  for (int q = 0; q < 4; ++q) {
+    const u32x2 c = row_codes(e.v[q], (uint32_t)code);
+    w[2 * q] = (int)c[0];
+    w[2 * q + 1] = (int)c[1];
   }
   return w;
 }

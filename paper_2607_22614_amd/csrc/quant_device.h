@@ -1,4 +1,4 @@
-// Device helpers of the 8-bit kernels: scales, rounding to e4m3, loads of 8 elements.
+// Device helpers of the 8-bit and gradient kernels: scales, rounding to e4m3, loads and stores of 8 elements.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -32,68 +32,139 @@ __device__ __forceinline__ uint32_t max_rows(uint32_t v) {
   return max(v, (uint32_t)__shfl_xor((int)v, 32));
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-// |v| as bits, 0 where v is not finite.
-__device__ __forceinline__ uint32_t finite_bits(float v) {
-  const uint32_t u = abs_bits(v);
-  return u < kInfBits ? u : 0u;
-}
-
-// e8m0 code of the smallest power of two, at least 2^-127, by which amax is at most 448 = 1.75 * 2^8:
+// e8m0 code of the smallest power of two, at least 2^-127, by which amax (its bits) is at most 448 = 1.75 * 2^8:
 // the exponent less 8, one more where the mantissa passes 1.75.  1 for amax = 0.
 __device__ __forceinline__ uint32_t scale_code(uint32_t amax) {
   const int c = (int)((amax + 0x1FFFFFu) >> 23) - 8;
   return amax == 0 ? 127u : (uint32_t)max(c, 0);
 }
-// 2^(127 - code), the factor that divides by the scale: exact, since code is at most 247.
-__device__ __forceinline__ float inverse_scale(uint32_t code) { return __uint_as_float((254u - code) << 23); }
+// The scale as an operand of the converts, which look at its exponent bits only (0 is 2^-127 to them).
+__device__ __forceinline__ float scale_operand(uint32_t code) { return __uint_as_float(code << 23); }
 
-// Four values times `inv` as e4m3 codes, rounded to even by the hardware convert.  Values are within
-// 448 after scaling; CHECK: some may not be finite, and those become NaN.
-template <bool CHECK>
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inv) {
-  if (CHECK) {
-    const float nan = __uint_as_float(0x7FC00000u);
-    a = abs_bits(a) < kInfBits ? a : nan;
-    b = abs_bits(b) < kInfBits ? b : nan;
-    c = abs_bits(c) < kInfBits ? c : nan;
-    d = abs_bits(d) < kInfBits ? d : nan;
-  }
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
-}
-
-// Elements [0, n) of the 8 at p, n <= 8; the others are 0.  vec: 16-byte loads where all 8 are there.
+// 8 elements of a row as they lie in memory.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t at, int n, bool vec, float (&v)[8]) {
+struct Raw8 {
+  u32x4 w[BF16 ? 1 : 2];
+};
+
+// Elements [0, n) of the 8 at `at`, n <= 8; the others are 0.  vec: 16-byte loads where all 8 are there.
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> load_raw8(const void* base, int64_t at, int n, bool vec) {
+  Raw8<BF16> v = {};
   if (BF16) {
     const uint16_t* p = static_cast<const uint16_t*>(base) + at;
     if (vec && n >= 8) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+      v.w[0] = *reinterpret_cast<const u32x4*>(p);
+    } else if (n > 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float((uint32_t)p[i] << 16) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (i < n) v.w[0][i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
     }
   } else {
-    const float* p = static_cast<const float*>(base) + at;
+    const uint32_t* p = static_cast<const uint32_t*>(base) + at;
     if (vec && n >= 8) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+      v.w[0] = *reinterpret_cast<const u32x4*>(p);
+      v.w[BF16 ? 0 : 1] = *reinterpret_cast<const u32x4*>(p + 4);
+    } else if (n > 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = a[i];
-        v[4 + i] = b[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (i < n) v.w[BF16 ? 0 : i / 4][i % 4] = p[i];
     }
   }
+  return v;
+}
+
+// fp32 bits of element i.
+template <bool BF16>
+__device__ __forceinline__ uint32_t bits_of(const Raw8<BF16>& v, int i) {
+  if (!BF16) return v.w[BF16 ? 0 : i / 4][i % 4];
+  const uint32_t w = v.w[0][i / 2];
+  return i % 2 ? w & 0xFFFF0000u : w << 16;
+}
+
+// Magnitudes of two elements at a time for bf16 (packed 16-bit maxima), of one for fp32.  finite: those that are not
+// finite count as 0.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+template <bool BF16>
+__device__ __forceinline__ uint32_t magnitude(uint32_t w, bool finite) {
+  if (BF16) {
+    w &= 0x7FFF7FFFu;
+    if (finite) {
+      if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+      if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+    }
+    return w;
+  }
+  w &= 0x7FFFFFFFu;
+  return finite && w >= kInfBits ? 0u : w;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  if (BF16) return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+  return max(a, b);
+}
+// Largest of the packed magnitudes, as fp32 bits.
+template <bool BF16>
+__device__ __forceinline__ uint32_t unpack_max(uint32_t m) {
+  return BF16 ? max(m << 16, m & 0xFFFF0000u) : m;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t row_max(const Raw8<BF16>& v, bool finite) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < (BF16 ? 4 : 8); ++i) m = larger<BF16>(m, magnitude<BF16>(v.w[BF16 ? 0 : i / 4][i % 4], finite));
+  return unpack_max<BF16>(m);
+}
+
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+// Four values over the scale as e4m3 codes: the hardware converts divide by the power of two exactly, round to even and
+// make NaN of what is not finite.  Values are within 448 after scaling.
+__device__ __forceinline__ uint32_t to_e4m3_f32(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {
+  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, __uint_as_float(a), __uint_as_float(b), scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __uint_as_float(c), __uint_as_float(d), scale, true);
+  return __builtin_bit_cast(uint32_t, w);
+}
+__device__ __forceinline__ uint32_t to_e4m3_bf16(uint32_t ab, uint32_t cd, float scale) {
+  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, ab), scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, cd), scale, true);
+  return __builtin_bit_cast(uint32_t, w);
+}
+
+// Codes of 8 elements of a row.
+template <bool BF16>
+__device__ __forceinline__ u32x2 row_codes(const Raw8<BF16>& v, uint32_t code) {
+  const float s = scale_operand(code);
+  if (BF16) return u32x2{to_e4m3_bf16(v.w[0][0], v.w[0][1], s), to_e4m3_bf16(v.w[0][2], v.w[0][3], s)};
+  const u32x4 a = v.w[0], b = v.w[BF16 ? 0 : 1];
+  return u32x2{to_e4m3_f32(a[0], a[1], a[2], a[3], s), to_e4m3_f32(b[0], b[1], b[2], b[3], s)};
+}
+
+// Codes of column j of 8 rows.
+template <bool BF16>
+__device__ __forceinline__ u32x2 column_codes(const Raw8<BF16> (&v)[8], int j, uint32_t code) {
+  const float s = scale_operand(code);
+  u32x2 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (BF16) {
+      uint32_t pair[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)  // (lower, upper) halves of two rows side by side
+        pair[i] = __builtin_amdgcn_perm(v[4 * h + 2 * i + 1].w[0][j / 2], v[4 * h + 2 * i].w[0][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+      r[h] = to_e4m3_bf16(pair[0], pair[1], s);
+    } else {
+      r[h] = to_e4m3_f32(bits_of<BF16>(v[4 * h], j), bits_of<BF16>(v[4 * h + 1], j), bits_of<BF16>(v[4 * h + 2], j), bits_of<BF16>(v[4 * h + 3], j), s);
+    }
+  }
+  return r;
+}
+
+// The same as fp32.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* base, int64_t at, int n, bool vec, float (&v)[8]) {
+  const Raw8<BF16> w = load_raw8<BF16>(base, at, n, vec);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(bits_of<BF16>(w, i));
 }
 
 // fp32 -> bf16, ties to even (the hardware convert).

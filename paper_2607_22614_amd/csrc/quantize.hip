@@ -21,52 +21,34 @@ struct QuantizeArgs {
 };
 
 // Blocks of 1 x 128, rows only.  A wave takes 512 columns (four blocks, 16 lanes each, 8 elements a lane) of
-// kRowsPerWave rows, whose loads are all in flight together; a block's maximum is a DPP reduction over its 16
+// ROWS rows, whose loads are all in flight together; a block's maximum is a DPP reduction over its 16
 // lanes, and the four codes of a row make the 32-bit word that one lane stores.
-constexpr int kRowsPerWave = 8;
 constexpr int kRowWaves = 4;
 
-template <bool BF16>
+template <bool BF16, int ROWS>
 __global__ __launch_bounds__(64 * kRowWaves) void quantize_rows_kernel(QuantizeArgs a) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   const uint32_t quad = blockIdx.x % a.tiles_x;
-  const uint32_t row0 = (blockIdx.x / a.tiles_x * kRowWaves + wave) * kRowsPerWave;
+  const uint32_t row0 = (blockIdx.x / a.tiles_x * kRowWaves + wave) * ROWS;
   if (row0 >= a.rows) return;
   const uint32_t col = quad * 512 + lane * 8;
   const int n = max(0, min(8, (int)a.cols - (int)col));
-  float v[kRowsPerWave][8];
+  Raw8<BF16> v[ROWS];
 #pragma unroll
-  for (int i = 0; i < kRowsPerWave; ++i)
-    load8<BF16>(a.src, (int64_t)min(row0 + i, a.rows - 1) * a.src_stride + col, n, a.vec, v[i]);
+  for (int i = 0; i < ROWS; ++i) v[i] = load_raw8<BF16>(a.src, (int64_t)min(row0 + i, a.rows - 1) * a.src_stride + col, n, a.vec);
   uint32_t word = 0;
 #pragma unroll
-  for (int i = 0; i < kRowsPerWave; ++i) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i][j]));
-    m = max16(m);
-    const bool odd = __any(m >= kInfBits);
-    if (odd) {
-      m = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = max(m, finite_bits(v[i][j]));
-      m = max16(m);
-    }
-    const uint32_t code = scale_code(m);
-    const float inv = inverse_scale(code);
-    u32x2 w;
-    if (odd) {
-      w = u32x2{to_e4m3<true>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<true>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
-    } else {
-      w = u32x2{to_e4m3<false>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<false>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
-    }
+  for (int i = 0; i < ROWS; ++i) {
+    uint32_t m = row_max(v[i], false);
+    if (__any(m >= kInfBits)) m = row_max(v[i], true);
+    const uint32_t code = scale_code(max16(m));
     const uint32_t codes = (uint32_t)__builtin_amdgcn_readlane((int)code, 0) | (uint32_t)__builtin_amdgcn_readlane((int)code, 16) << 8 |
                            (uint32_t)__builtin_amdgcn_readlane((int)code, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)code, 48) << 24;
     if ((int)lane == i) word = codes;
     if (row0 + i < a.rows && (col & ~127u) < a.cols)
-      *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = w;
+      *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = row_codes(v[i], code);
   }
-  if (lane < kRowsPerWave && row0 + lane < a.rows)
+  if (lane < ROWS && row0 + lane < a.rows)
     reinterpret_cast<uint32_t*>(a.q.scales)[(int64_t)quad * a.rows + row0 + lane] = word;
 }
 
@@ -92,30 +74,26 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   const uint32_t ct = blockIdx.x % a.tiles_x, rt = blockIdx.x / a.tiles_x;
   const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * 8;
   const int n = max(0, min(8, (int)a.cols - (int)col));
-  float v[8][8];
+  Raw8<BF16> v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const bool in = row0 + i < a.rows;
-    load8<BF16>(a.src, (int64_t)(in ? row0 + i : a.rows - 1) * a.src_stride + col, in ? n : 0, a.vec, v[i]);
+    v[i] = load_raw8<BF16>(a.src, (int64_t)(in ? row0 + i : a.rows - 1) * a.src_stride + col, in ? n : 0, a.vec);
   }
-  uint32_t top = 0;
+  // the lane's largest magnitude of each row; finite ones only if any is not
+  uint32_t rmax[8], top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[i][j]));
+  for (int i = 0; i < 8; ++i) top = max(top, rmax[i] = row_max(v[i], false));
   const bool odd = __any(top >= kInfBits);
+  if (odd) {
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, rmax[i] = row_max(v[i], true));
+  }
 
   uint32_t square_code = 0;
   if (SQUARE) {
-    uint32_t m = top;
-    if (odd) {
-      m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, finite_bits(v[i][j]));
-    }
-    m = max_rows(max16(m));
+    const uint32_t m = max_rows(max16(top));
     if ((tid & 63) == 0) cmax[0][wave] = m;
     __syncthreads();
     square_code = scale_code(max(max(cmax[0][0], cmax[0][1]), max(cmax[0][2], cmax[0][3])));
@@ -128,21 +106,9 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   if (ROWS) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      uint32_t code = square_code;
-      if (!SQUARE) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, odd ? finite_bits(v[i][j]) : abs_bits(v[i][j]));
-        code = scale_code(max16(m));
-      }
-      const float inv = inverse_scale(code);
-      u32x2 w;
-      if (odd)
-        w = u32x2{to_e4m3<true>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<true>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
-      else
-        w = u32x2{to_e4m3<false>(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3<false>(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+      const uint32_t code = SQUARE ? square_code : scale_code(max16(rmax[i]));
       if (row0 + i < a.rows) {
-        *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = w;
+        *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = row_codes(v[i], code);
         if (!SQUARE && tx == 0) put_code(a.q, row0 + i, ct, code);
       }
     }
@@ -155,12 +121,20 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
       for (int j = 0; j < 8; ++j) code[j] = square_code;
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int w = 0; w < (BF16 ? 4 : 8); ++w) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, odd ? finite_bits(v[i][j]) : abs_bits(v[i][j]));
-        m = max_rows(m);
-        if ((tid & 63) < 16) cmax[wave][tx * 8 + j] = m;
+        for (int i = 0; i < 8; ++i) m = larger<BF16>(m, magnitude<BF16>(v[i].w[BF16 ? 0 : w / 4][w % 4], odd));
+        m = larger<BF16>(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = larger<BF16>(m, (uint32_t)__shfl_xor((int)m, 32));
+        if ((tid & 63) < 16) {
+          if (BF16) {
+            cmax[wave][tx * 8 + 2 * w] = m << 16;
+            cmax[wave][tx * 8 + 2 * w + 1] = m & 0xFFFF0000u;
+          } else {
+            cmax[wave][tx * 8 + w] = m;
+          }
+        }
       }
       __syncthreads();
 #pragma unroll
@@ -171,15 +145,8 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
       }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float inv = inverse_scale(code[j]);
-      u32x2 w;
-      if (odd)
-        w = u32x2{to_e4m3<true>(v[0][j], v[1][j], v[2][j], v[3][j], inv), to_e4m3<true>(v[4][j], v[5][j], v[6][j], v[7][j], inv)};
-      else
-        w = u32x2{to_e4m3<false>(v[0][j], v[1][j], v[2][j], v[3][j], inv), to_e4m3<false>(v[4][j], v[5][j], v[6][j], v[7][j], inv)};
-      *reinterpret_cast<u32x2*>(turned + (tx * 8 + j) * 128 + ((ty ^ tx) * 8)) = w;
-    }
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<u32x2*>(turned + (tx * 8 + j) * 128 + ((ty ^ tx) * 8)) = column_codes(v, j, code[j]);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -193,14 +160,26 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   }
 }
 
+// Eight rows a wave keep the loads of a long matrix in flight; where that leaves CUs without work, one.
+template <bool BF16>
+void launch_rows(const QuantizeArgs& a, hipStream_t st) {
+  const uint32_t grid8 = a.tiles_x * (uint32_t)ceil_div(a.rows, 8 * kRowWaves);
+  if (grid8 >= 512)
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, 8>), dim3(grid8), dim3(64 * kRowWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL((quantize_rows_kernel<BF16, 1>), dim3(a.tiles_x * (uint32_t)ceil_div(a.rows, kRowWaves)), dim3(64 * kRowWaves), 0, st, a);
+}
+
 template <bool BF16, bool SQUARE>
 void launch_tiles(const QuantizeArgs& a, dim3 grid, hipStream_t st) {
-  if (a.q.data && a.qt.data)
-    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, true>), grid, dim3(256), 0, st, a);
-  else if (a.q.data)
-    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, false>), grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, false, true>), grid, dim3(256), 0, st, a);
+  const dim3 block(256);
+  if (a.q.data && a.qt.data) {
+    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, true>), grid, block, 0, st, a);
+  } else if (a.qt.data) {
+    hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, false, true>), grid, block, 0, st, a);
+  } else {
+    if constexpr (SQUARE) hipLaunchKernelGGL((quantize_tile_kernel<BF16, true, true, false>), grid, block, 0, st, a);
+  }
 }
 
 }  // namespace
@@ -217,11 +196,8 @@ hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
   const bool square = (l.q.data ? l.q.sh : l.qt.sh) != 0;
   if (!square && !l.qt.data) {
     a.tiles_x = (uint32_t)ceil_div(l.cols, 512);
-    const uint32_t grid = a.tiles_x * (uint32_t)ceil_div(l.rows, kRowsPerWave * kRowWaves);
-    if (l.bf16)
-      hipLaunchKernelGGL(quantize_rows_kernel<true>, dim3(grid), dim3(64 * kRowWaves), 0, st, a);
-    else
-      hipLaunchKernelGGL(quantize_rows_kernel<false>, dim3(grid), dim3(64 * kRowWaves), 0, st, a);
+    if (l.bf16) launch_rows<true>(a, st);
+    else launch_rows<false>(a, st);
     return hipGetLastError();
   }
   a.tiles_x = (uint32_t)ceil_div(l.cols, 128);

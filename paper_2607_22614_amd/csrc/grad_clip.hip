@@ -73,19 +73,41 @@ __device__ __forceinline__ double block_sum(double v, double (&red)[kThreadsG / 
   return s;
 }
 
-__device__ __forceinline__ void add_square(double (&acc)[2], float v, int i) {
-  const double d = v;
-  acc[i & 1] = fma(d, d, acc[i & 1]);
+// fp32 values of element i of the 4 or 8 in 16 bytes.
+template <bool BF16>
+__device__ __forceinline__ float value(u32x4 w, int i) {
+  return __uint_as_float(!BF16 ? w[BF16 ? 0 : i] : i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
+
+// Whole chunks move 16 bytes per lane and access, kAhead of them in flight.
+constexpr int kAhead = 8;
 
 template <bool BF16>
 __device__ __forceinline__ void sum_chunk(const void* grad, uint64_t at, uint32_t n, double (&acc)[2]) {
+  constexpr int E = BF16 ? 8 : 4;
+  if (n == kGradChunk && aligned16(grad)) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(grad) + at * (BF16 ? 2 : 4)) + threadIdx.x;
+#pragma unroll
+    for (uint32_t i = 0; i < kGradChunk / (kThreadsG * E * kAhead); ++i) {
+      u32x4 w[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) w[k] = load_stream(p + (i * kAhead + k) * kThreadsG);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const double d = value<BF16>(w[k], j);
+          acc[j & 1] = fma(d, d, acc[j & 1]);
+        }
+    }
+    return;
+  }
   const bool vec = aligned16(grad);
   for (uint32_t i = threadIdx.x * 8; i < n; i += kThreadsG * 8) {
     float v[8];
     load8<BF16>(grad, (int64_t)(at + i), (int)min(8u, n - i), vec, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) add_square(acc, v[j], j);
+    for (int j = 0; j < 8; ++j) acc[j & 1] = fma((double)v[j], (double)v[j], acc[j & 1]);
   }
 }
 
@@ -120,7 +142,38 @@ __global__ __launch_bounds__(kThreadsG) void grad_total_kernel(const double* sum
 
 template <bool BF16, bool OUT_BF16>
 __device__ __forceinline__ void scale_chunk(const void* grad, void* out, uint64_t at, uint32_t n, double f) {
+  constexpr int E = BF16 ? 8 : 4;
   const bool vec = aligned16(grad), ovec = aligned16(out);
+  if (n == kGradChunk && vec && ovec) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(grad) + at * (BF16 ? 2 : 4)) + threadIdx.x;
+    uint8_t* q = static_cast<uint8_t*>(out) + at * (OUT_BF16 ? 2 : 4);
+#pragma unroll
+    for (uint32_t i = 0; i < kGradChunk / (kThreadsG * E * kAhead); ++i) {
+      u32x4 w[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) w[k] = load_stream(p + (i * kAhead + k) * kThreadsG);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        float v[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = (float)(value<BF16>(w[k], j) * f);
+        const uint32_t to = ((i * kAhead + k) * kThreadsG + threadIdx.x) * E;  // element
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+          if constexpr (OUT_BF16) {
+            if constexpr (BF16) {
+              if (j == 0) store_stream(u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[E - 4], v[E - 3]), bf16_pair(v[E - 2], v[E - 1])}, reinterpret_cast<u32x4*>(q + 2 * to));
+            } else {
+              store_stream(u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, reinterpret_cast<u32x2*>(q + 2 * to));
+            }
+          } else {
+            store_stream(f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]}, reinterpret_cast<f32x4*>(q + 4 * (to + j)));
+          }
+        }
+      }
+    }
+    return;
+  }
   for (uint32_t i = threadIdx.x * 8; i < n; i += kThreadsG * 8) {
     float v[8];
     const int k = (int)min(8u, n - i);

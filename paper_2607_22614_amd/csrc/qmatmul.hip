@@ -25,7 +25,7 @@ struct ProductArgs {
   int64_t c_stride;
   uint32_t m, n, kb, tiles_m, tiles_n;
   uint32_t splits;  // of the blocks: workgroups of one tile, whose fp32 sums go to part[split][m][part_stride]
-  int32_t x_vec, c_vec, c_bf16, accumulate;
+  int32_t c_vec, c_bf16, accumulate;
   float* part;
   int64_t part_stride;
 };
@@ -116,20 +116,40 @@ __device__ __forceinline__ void store_piece(const ProductArgs& p, uint32_t m, ui
   }
 }
 
-// A lane's 32 elements of 128 columns of one row of x (X: 1 fp32, 2 bf16), as they lie in memory.
+// A lane's 32 elements of 128 columns of one row of x, as they lie in memory.  How x comes: fp32 or bf16, in rows of whole
+// 16-byte pieces (kVec: loads without branches, which the compiler leaves in flight) or any rows; or as codes.
+enum XKind { kCodes = 0, kF32 = 1, kBf16 = 2, kVec = 4 };
 template <int X>
 struct Elements {
-  Raw8<X == 2> v[X == 0 ? 1 : 4];
+  Raw8<(X & kBf16) != 0> v[X == kCodes ? 1 : 4];
 };
 template <int X>
 __device__ __forceinline__ Elements<X> load_elements(const ProductArgs& p, uint32_t row, uint32_t col) {
+  constexpr bool BF16 = (X & kBf16) != 0;
   Elements<X> e;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t c = col + (q >> 1) * 64 + (q & 1) * 8;
-    e.v[q] = load_raw8<X == 2>(p.x, (int64_t)row * p.x_stride + c, max(0, min(8, (int)p.a.cols - (int)c)), p.x_vec);
+    const int64_t at = (int64_t)row * p.x_stride;
+    if (X & kVec) {
+      const u32x4* x = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.x) + (at + min(c, p.a.cols - 8)) * (BF16 ? 2 : 4));
+#pragma unroll
+      for (int i = 0; i < (BF16 ? 1 : 2); ++i) e.v[q].w[i] = x[i];
+    } else {
+      e.v[q] = load_raw8<BF16>(p.x, at + c, max(0, min(8, (int)p.a.cols - (int)c)), false);
+    }
   }
   return e;
+}
+// Zeros in place of what kVec loads read again from columns that are not there (pieces are all there or not at all).
+template <int X>
+__device__ __forceinline__ void clear_beyond(const ProductArgs& p, uint32_t col, Elements<X>& e) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int i = 0; i < ((X & kBf16) ? 1 : 2); ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) e.v[q].w[i][w] = col + (q >> 1) * 64 + (q & 1) * 8 < p.a.cols ? e.v[q].w[i][w] : 0u;
 }
 
 // Their codes, and the scale of the row's 128 columns, as dr_quantize gives them.
@@ -155,9 +175,8 @@ __device__ __forceinline__ i32x8 quantize_block(const Elements<X>& e, int& code)
 }
 
 // Few rows: a tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
-// instructions; the KS waves of the workgroup take the 128-column blocks in turn, each loading its next block while it
-// multiplies one, and join their sums in LDS, in the order of the waves.  X: 0 takes a from its codes, 1 quantizes fp32
-// rows of x, 2 bf16 rows.
+// instructions; the KS waves of the workgroup take the 128-column blocks in turn, each with its next block in flight while
+// it multiplies one, and join their sums in LDS, in the order of the waves.  X: a's codes, or rows of x to quantize.
 template <int FT, int TT, int KS, int X, bool FAST>
 __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) {
   __shared__ f32x4 part[KS][FT * TT][64];
@@ -202,36 +221,43 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
     return k;
   };
   f32x4 acc[FT][TT] = {};
+  auto multiply = [&](Block& k, uint32_t j) {
+    i32x8 aw[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      if constexpr (X != 0) {
+        if ((X & kVec) && j * 128 + 128 > p.a.cols) clear_beyond<X>(p, j * 128 + g * 16, k.x[t]);
+        aw[t] = quantize_block(k.x[t], k.ea[t]);
+      } else {
+        aw[t] = k.a[t];
+      }
+    }
+    if constexpr (FAST) {
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.b[f], aw[t], acc[f][t], 0, 0, 0, k.eb[f], 0, k.ea[t]);
+    } else {
+      Bf16Codes ca[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) ca[t] = to_bf16(aw[t], k.ea[t]);
+#pragma unroll
+      for (int f = 0; f < FT; ++f) {
+        const Bf16Codes cb = to_bf16(k.b[f], k.eb[f]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.v[i], ca[t].v[i], acc[f][t], 0, 0, 0);
+      }
+    }
+  };
   if (wave < p.kb) {
     Block next = load(wave);
     for (uint32_t j = wave; j < p.kb; j += KS) {
       Block k = next;
-      next = load(min(j + KS, p.kb - 1));
-      i32x8 aw[TT];
-#pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        if constexpr (X != 0) aw[t] = quantize_block(k.x[t], k.ea[t]);
-        else aw[t] = k.a[t];
-      }
-      if constexpr (FAST) {
-#pragma unroll
-        for (int f = 0; f < FT; ++f)
-#pragma unroll
-          for (int t = 0; t < TT; ++t)
-            acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.b[f], aw[t], acc[f][t], 0, 0, 0, k.eb[f], 0, k.ea[t]);
-      } else {
-        Bf16Codes ca[TT];
-#pragma unroll
-        for (int t = 0; t < TT; ++t) ca[t] = to_bf16(aw[t], k.ea[t]);
-#pragma unroll
-        for (int f = 0; f < FT; ++f) {
-          const Bf16Codes cb = to_bf16(k.b[f], k.eb[f]);
-#pragma unroll
-          for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.v[i], ca[t].v[i], acc[f][t], 0, 0, 0);
-        }
-      }
+      if (j + KS < p.kb) next = load(j + KS);
+      multiply(k, j);
     }
   }
 #pragma unroll
@@ -253,6 +279,17 @@ void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
   const dim3 grid(a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16)), block(64 * KS);
   if (fast) hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, false>), grid, block, 0, st, a);
+}
+
+// More columns a workgroup read a fewer times, fewer columns give more workgroups.  One tile of 16 columns up to 4096
+// (256 workgroups), two up to 16384, then four; eight waves share the blocks, four of the widest.  In us for 1 / 2 / 4:
+//   1 row, 4096 x 3584: 5.5 / 7.1 / 10.4     16 rows, 6912 x 5120: 17.0 / 13.0 / 18.3     32 rows, 32064 x 4096: 50 / 37 / 32
+// and with 4 / 8 / 16 waves, 1 row, 4096 x 3584: 6.4 / 5.5 / 5.7; four tiles, 16 rows, 151936 x 896: 29 / 38 / 66.
+template <int TT, int X>
+void launch_few_rows(const ProductArgs& a, bool fast, hipStream_t st) {
+  if (a.n <= 4096) launch_direct<1, TT, 8, X>(a, fast, st);
+  else if (a.n <= 16384) launch_direct<2, TT, 8, X>(a, fast, st);
+  else launch_direct<4, TT, 4, X>(a, fast, st);
 }
 
 // ------------------------------------------------------------------ large products
@@ -503,13 +540,19 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   a.m = l.m;
   a.n = l.n;
   a.kb = l.kb;
-  a.x_vec = l.x_aligned;
   a.c_vec = reinterpret_cast<uintptr_t>(l.c) % 16 == 0 && l.c_stride * (l.c_bf16 ? 2 : 4) % 16 == 0;
   a.c_bf16 = l.c_bf16;
   a.accumulate = l.accumulate;
   if (l.x) {
-    if (l.x_bf16) launch_direct<1, 1, 8, 2>(a, l.fast, st);
-    else launch_direct<1, 1, 8, 1>(a, l.fast, st);
+    // rows that are no whole 16-byte pieces are loaded element by element, by one form of the kernel
+    const bool vec = l.x_aligned && l.a.cols % 8 == 0;
+    if (l.x_bf16) {
+      if (vec) launch_few_rows<1, kBf16 | kVec>(a, l.fast, st);
+      else launch_direct<1, 1, 8, kBf16>(a, l.fast, st);
+    } else {
+      if (vec) launch_few_rows<1, kF32 | kVec>(a, l.fast, st);
+      else launch_direct<1, 1, 8, kF32>(a, l.fast, st);
+    }
   } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect) {
     a.splits = plan.splits;
     a.part = static_cast<float*>(l.workspace);
@@ -517,10 +560,8 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
     if (plan.kind == ProductPlan::kTile256) launch_tile<256, 256, 2, 2>(a, l.fast, st);
     else launch_tile<128, 128, 2, 2>(a, l.fast, st);
   } else {
-    if (l.m <= 16) launch_direct<2, 1, 8, 0>(a, l.fast, st);
-    else if (l.m <= 32) launch_direct<2, 2, 8, 0>(a, l.fast, st);
-    else if (l.m <= 48) launch_direct<2, 3, 8, 0>(a, l.fast, st);
-    else launch_direct<2, 4, 8, 0>(a, l.fast, st);
+    if (l.m <= 16) launch_few_rows<1, kCodes>(a, l.fast, st);
+    else launch_few_rows<2, kCodes>(a, l.fast, st);
   }
   return hipGetLastError();
 }

@@ -239,11 +239,24 @@ def _shards(xs: Sequence, count: int, nbytes: int, where: str) -> ctypes.Array:
                                        for i, x in enumerate(xs)])
 
 
+_current = None  # () -> the current stream's handle, without a Stream object around it where torch has a call for that
+
+
+def _find_current():
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    torch.cuda.current_device()  # initialises torch's side of the GPU
+    if raw and device:
+        return lambda: raw(device())
+    return lambda: torch.cuda.current_stream().cuda_stream
+
+
 def _stream(stream) -> int:
+    global _current
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object around it
-        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+        if _current is None:
+            _current = _find_current()
+        return _current()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -526,27 +539,37 @@ def dr_break_even_steps(switch_cost_s: float, step_before_s: float, step_after_s
 
 
 # ------------------------------------------------------------------ 8-bit matrices
+_TYPES: dict = {}  # torch dtype -> DR_TYPE_*, filled at the first tensor
+
+
 def _type(t, where: str) -> int:
     """DR_TYPE_* of a tensor."""
-    import torch
-    if t.dtype is torch.bfloat16:
-        return DR_TYPE_BF16
-    if t.dtype is torch.float32:
-        return DR_TYPE_F32
-    raise ValueError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        import torch
+        _TYPES.update({torch.float32: DR_TYPE_F32, torch.bfloat16: DR_TYPE_BF16})
+        kind = _TYPES.get(t.dtype)
+        if kind is None:
+            raise ValueError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+    return kind
 
 
 def _dense_rows(t, where: str):
     """(address, type, rows, cols, row stride) of a 2-d device tensor whose rows are dense."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{where}: expected a 2-d device tensor, got {t.dim()}-d on {t.device}")
-    rows, cols = t.shape
-    step, inner = t.stride()
-    if inner != 1 and cols > 1:
-        raise ValueError(f"{where}: the elements of a row are not adjacent")
-    if step < cols and rows > 1:
-        raise ValueError(f"{where}: rows overlap")
-    return t.data_ptr(), _type(t, where), rows, cols, step if rows > 1 else max(step, cols)
+    rows, cols = shape
+    step = cols
+    if not t.is_contiguous():
+        step, inner = t.stride()
+        if inner != 1 and cols > 1:
+            raise ValueError(f"{where}: the elements of a row are not adjacent")
+        if rows == 1:
+            step = max(step, cols)
+        elif step < cols:
+            raise ValueError(f"{where}: rows overlap")
+    return t.data_ptr(), _TYPES.get(t.dtype) or _type(t, where), rows, cols, step
 
 
 def dr_qmatrix_sizes(rows: int, cols: int, block_rows: int = 1) -> dict:
@@ -598,7 +621,9 @@ def _workspace(ws, where: str):
     """(address, bytes) of a workspace tensor or None."""
     if ws is None:
         return 0, 0
-    return (ws.data_ptr() if _fits(ws, 0) else _buf(ws, 0, where, True)), ws.nbytes
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError(f"{where}: expected a dense device tensor")
+    return ws.data_ptr(), ws.nbytes
 
 
 def dr_qmatmul(a: QMatrix, b: QMatrix, out, accumulate: bool = False, fast: bool = False, workspace=None,

@@ -201,6 +201,25 @@ def test_linear(m, n, k, dtype):
         _close(y, want, size, k, out_type == torch.bfloat16)
 
 
+@pytest.mark.parametrize("m", [1, 16, 20, 32])
+@pytest.mark.parametrize("n,k", [(4097, 264), (16385, 130), (20001, 1160)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_few_rows_of_wide_weights(m, n, k, fast):
+    dr = _dr()
+    say("few rows, wide", m, n, k, fast)
+    gen = torch.Generator().manual_seed(m + n)
+    w, wv = _matrix(dr, n, k, 128, n, spread=3)
+    for dtype in (torch.bfloat16, torch.float32):
+        x = torch.randn((m, k), generator=gen).to(dtype)
+        xv = quant.values(*quant.quantize(x.to(torch.float64).numpy(), 1), k, 1)
+        want, size = quant.product(xv, wv)
+        y = torch.empty((m, n), device="cuda")
+        dr.dr_qlinear(x.cuda(), w, y, fast=fast, workspace=torch.empty((dr.dr_qlinear_workspace(m, w),), dtype=torch.uint8, device="cuda"))
+        if fast:  # 2^-10 of each group's largest product, at most of the sum of magnitudes
+            size = size * (1 + 2.0**-10 / ((-(-k // 128) * 128 + 64) * 2.0**-23))
+        _close(y, want, size, k, False)
+
+
 @pytest.mark.parametrize("m", [3, 40])
 def test_linear_rows_at_any_element_and_not_finite(m):
     dr = _dr()

@@ -622,7 +622,7 @@ int dr_qlinear_workspace(int64_t m, int64_t n, int64_t k, uint64_t* bytes);
  * write, numel elements of out_type at `out`: its own place (the flat buffer
  * of the training layout, say) or `grad` itself with the same type.  Device
  * pointers, aligned to their element type (16 bytes is fastest); numel >= 0
- * and at most 2^45 in all.  The list is host memory, read during the call only.
+ * and at most 2^42 in all.  The list is host memory, read during the call only.
  */
 typedef struct {
   const void* grad;

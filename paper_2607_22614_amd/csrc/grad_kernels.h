@@ -10,8 +10,10 @@
 
 namespace dr {
 
-constexpr int64_t kMaxGradElems = 1ll << 45;  // of a list: its chunks are counted in 32 bits
-constexpr uint32_t kGradSums = 2048;  // workgroups of a launch, and sums in the workspace
+constexpr int64_t kMaxGradElems = 1ll << 42;  // of a list: its chunks are counted in 32 bits
+constexpr uint32_t kGradSums = 2048;  // workgroups of a launch of the norm, and its sums in the workspace
+// The most sums that every workgroup of the scaling adds up itself.
+constexpr uint32_t kFewSums = kGradSums / 2;
 
 // One sum of squares per workgroup into partial[0 .. *nsums), *nsums <= kGradSums (0: an empty list).
 hipError_t launch_grad_norm(const dr_grad* grads, int64_t count, double* partial, uint32_t* nsums, hipStream_t st);

@@ -21,7 +21,7 @@ int check_list(const dr_grad* grads, int64_t count, bool out, const char* what) 
     const int size = element_bytes(g.grad_type), out_size = element_bytes(g.out_type);
     if (!size || (out && !out_size)) return fail(DR_EINVAL, "%s: gradient %lld has an unknown type", what, (long long)i);
     if (g.numel < 0 || g.numel > kMaxGradElems || (all += (uint64_t)g.numel) > (uint64_t)kMaxGradElems)
-      return fail(DR_EINVAL, "%s: gradient %lld: %lld elements (at most 2^45 in all)", what, (long long)i, (long long)g.numel);
+      return fail(DR_EINVAL, "%s: gradient %lld: %lld elements (at most 2^42 in all)", what, (long long)i, (long long)g.numel);
     if (!g.numel) continue;
     if (!aligned(g.grad, size) || (out && !aligned(g.out, out_size)))
       return fail(DR_EINVAL, "%s: gradient %lld: pointer null or misaligned", what, (long long)i);
@@ -47,7 +47,7 @@ using namespace dr;
 extern "C" int dr_grad_workspace(uint64_t* bytes) {
   clear_error();
   if (!bytes) return fail(DR_EINVAL, "dr_grad_workspace: null argument");
-  *bytes = kGradSums * sizeof(double);
+  *bytes = (kGradSums + 1) * sizeof(double);  // and their total
   return DR_OK;
 }
 
@@ -91,6 +91,12 @@ extern "C" int dr_grad_clip(const dr_grad* grads, int64_t count, double max_norm
   double* partial = static_cast<double*>(workspace);
   uint32_t nsums = 0;
   hipError_t e = launch_grad_norm(grads, count, partial, &nsums, st);
-  if (e == hipSuccess) e = launch_grad_scale(grads, count, partial, nsums, max_norm, norm_out, st);
+  const double* sums = partial;
+  if (e == hipSuccess && nsums > kFewSums) {
+    sums = partial + kGradSums;
+    e = launch_grad_total(partial, nsums, partial + kGradSums, nullptr, st);
+    nsums = 1;
+  }
+  if (e == hipSuccess) e = launch_grad_scale(grads, count, sums, nsums, max_norm, norm_out, st);
   return hip_result(e, what);
 }

@@ -8,7 +8,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "quant_device.h"
 
@@ -24,7 +23,8 @@ struct ProductArgs {
   void* c;
   int64_t c_stride;
   uint32_t m, n, kb, tiles_m, tiles_n;
-  uint32_t splits;  // of the blocks: workgroups of one tile, whose fp32 sums go to part[split][m][part_stride]
+  uint32_t splits;  // of the blocks: items of one tile, whose fp32 sums go to part[split][m][part_stride]
+  int64_t split_bytes;  // of c, from one split to the next (0 without them)
   int32_t c_vec, c_bf16, accumulate;
   float* part;
   int64_t part_stride;
@@ -75,36 +75,6 @@ __device__ __forceinline__ void store4(const ProductArgs& p, uint32_t m, uint32_
     }
   } else {
     float* c = static_cast<float*>(p.c) + at;
-    if (whole) {
-      f32x4* q = reinterpret_cast<f32x4*>(c);
-      *q = p.accumulate ? *q + v : v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n0 + i < p.n) c[i] = p.accumulate ? c[i] + v[i] : v[i];
-    }
-  }
-}
-
-// 16 bytes of results, columns n0 on, of row m of c.
-template <int BYTES>
-__device__ __forceinline__ void store_piece(const ProductArgs& p, uint32_t m, uint32_t n0, u32x4 w) {
-  constexpr int kElems = 16 / BYTES;
-  if (m >= p.m || n0 >= p.n) return;
-  const int64_t at = (int64_t)m * p.c_stride + n0;
-  const bool whole = p.c_vec && n0 + kElems <= p.n;
-  if (BYTES == 2) {
-    uint16_t* c = static_cast<uint16_t*>(p.c) + at;
-    if (whole) {
-      *reinterpret_cast<u32x4*>(c) = w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (n0 + i < p.n) c[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
-    }
-  } else {
-    float* c = static_cast<float*>(p.c) + at;
-    const f32x4 v = __builtin_bit_cast(f32x4, w);
     if (whole) {
       f32x4* q = reinterpret_cast<f32x4*>(c);
       *q = p.accumulate ? *q + v : v;
@@ -297,104 +267,186 @@ void launch_few_rows(const ProductArgs& a, bool fast, hipStream_t st) {
 // 16 bytes per lane from memory to LDS, at `to` + 16 * lane; nothing passes through registers.  As a buffer access its
 // address is the tile's base, the lane's offset and the step's, with no arithmetic in between.
 typedef __amdgpu_buffer_rsrc_t Buffer;
-__device__ __forceinline__ Buffer buffer_at(const uint8_t* base) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, 0xFFFFFFFFu, 0x00027000);  // raw, 32-bit data
+// What lies `bytes` and more behind its base is not read, and counts as 0.
+__device__ __forceinline__ Buffer buffer_at(const uint8_t* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00027000);  // raw, 32-bit data
 }
 __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lane_at, uint32_t at, uint8_t* to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)lane_at, (int)at, 0, 0);
 }
 
-// Tile (tm, tn) of workgroup b: each XCD takes a contiguous eighth of the tiles, in bands of kBand tiles down, so that
-// the workgroups running at once on it share rows of both operands in its L2.
-constexpr uint32_t kBand = 8;
-// Returns the split: whole products of tiles follow one another.
-__device__ __forceinline__ uint32_t tile_of(uint32_t b, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits, uint32_t& tm, uint32_t& tn) {
-  const uint32_t all = xcd_tile(b, tiles_m * tiles_n * splits), split = all / (tiles_m * tiles_n), t = all % (tiles_m * tiles_n);
-  const uint32_t band = t / (kBand * tiles_n), high = min(kBand, tiles_m - band * kBand), i = t - band * kBand * tiles_n;
-  tm = band * kBand + i % high;
-  tn = i / high;
-  return split;
+// Every wave's copies have landed, and all of them see that.  The wait is written out: a barrier alone orders the LDS
+// accesses that the compiler sees, and leaves copies to LDS on their way.
+__device__ __forceinline__ void landed_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), the other counters as they are
+  asm volatile("" ::: "memory");
+  __syncthreads();
 }
 
-// Results of a wave, TM * 32 rows by TN * 32 columns from (m0, n0), through TM * TN * 2 KiB of LDS.
-template <int TM, int TN, int BYTES>
+// Work item b of a product: the tile at (m0, n0) and its blocks [j0, j1), one split's.  Each XCD takes a contiguous eighth
+// of the items; the tiles of a split follow one another in bands of kBand tiles down, so that the workgroups running at
+// once on an XCD share rows of both operands in its L2.
+constexpr uint32_t kBand = 8;
+struct Item {
+  uint32_t m0, n0, split, j0, j1;
+};
+__device__ __forceinline__ uint32_t same(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+template <int BM, int BN>
+__device__ __forceinline__ Item item_of(const ProductArgs& p, uint32_t b) {
+  const uint32_t tiles = p.tiles_m * p.tiles_n, all = xcd_tile(b, tiles * p.splits), split = all / tiles, t = all % tiles;
+  const uint32_t band = t / (kBand * p.tiles_n), high = min(kBand, p.tiles_m - band * kBand), i = t - band * kBand * p.tiles_n;
+  // the same for the whole workgroup, which the compiler does not see behind the divisions
+  return Item{same((band * kBand + i % high) * BM), same(i / high * BN), same(split), same((uint32_t)((uint64_t)p.kb * split / p.splits)),
+              same((uint32_t)((uint64_t)p.kb * (split + 1) / p.splits))};
+}
+
+// Results of a wave, TM * 32 rows by TN * 32 columns from (m0, n0), through TN * 2 KiB of LDS of its own: 32 rows of all
+// columns in bf16 or of half of them in fp32 at a time, so that they leave as runs of whole lines.  A row's 16-byte pieces
+// lie at piece ^ row % pieces.  VEC: rows of c are whole 16-byte pieces and a lane stores one, else one element.
+//   Everything is one run of instructions without branches (the accumulators would leave their registers all at once
+// ahead of one): c is a buffer, what lies outside of it gets an offset past its end, and where nothing is accumulated
+// the buffer that c is read from is empty.
+// bf16_pair, but where it stands: the compiler would convert a wave's whole results at once, ahead of all parts.
+__device__ __forceinline__ uint32_t bf16_pair_here(float lo, float hi) {
+  uint32_t r;
+  asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(lo), "v"(hi));
+  return r;
+}
+
+constexpr uint32_t kOutside = 1u << 31;  // 128 rows of c lie within it (launch_product)
+template <int TM, int TN, int BYTES, bool VEC>
 __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 (&acc)[TN][TM], uint8_t* lds, uint32_t m0, uint32_t n0, uint32_t lane) {
-  constexpr int kPitch = TN * 32 * BYTES, kPiecesRow = kPitch / 16, kPart = TM * 2 / BYTES;  // tiles down that fit at once
-  constexpr int kMask = kPiecesRow - 1, kRowsAt = 64 / kPiecesRow, kElems = 16 / BYTES;
-  static_assert(kPiecesRow <= 64 && (kPiecesRow & kMask) == 0, "rows of a power of two of pieces");
-  const uint32_t r = lane & 31, g = lane >> 5;
+  constexpr int kXs = TN * 2 / BYTES, kPitch = TN * 64, kPiecesRow = kPitch / 16, kMask = kPiecesRow - 1, kElems = 16 / BYTES;
+  constexpr int kSize = VEC ? 16 : BYTES, kAcross = kPitch / kSize, kRowsAt = kAcross < 64 ? 64 / kAcross : 1, kTimes = 32 * kPitch / kSize / 64;
+  static_assert((kPiecesRow & kMask) == 0 && kXs * 32 * BYTES == kPitch, "rows of a power of two of pieces");
+  const uint32_t r = lane & 31, g = lane >> 5, row_bytes = (uint32_t)p.c_stride * BYTES;
+  const uint8_t* base = static_cast<const uint8_t*>(p.c) + ((int64_t)m0 * p.c_stride + n0) * BYTES;
+  const Buffer c = buffer_at(base, kOutside), old = buffer_at(base, p.accumulate ? kOutside : 0u);
 #pragma unroll
-  for (int y0 = 0; y0 < TM; y0 += kPart) {
+  for (int y = 0; y < TM; ++y)
 #pragma unroll
-    for (int x = 0; x < TN; ++x)
+    for (int x0 = 0; x0 < TN; x0 += kXs) {
+      __builtin_amdgcn_sched_barrier(0);  // one part at a time: the registers hold no more
+      uint32_t at[VEC ? kTimes : 1];
+      f32x4 before[VEC && BYTES == 4 ? kTimes : 1];
+      // offset in c of what the lane stores at time i, and its place in the LDS
+      auto place = [&](int i, uint32_t& from) {
+        const uint32_t unit = i * 64 + lane, row = unit / kAcross, col = unit % kAcross * (kSize / BYTES);
+        from = row * kPitch + ((col / kElems ^ (row & kMask)) * 16) + col % kElems * BYTES;
+        const bool in = m0 + y * 32 + row < p.m && n0 + x0 * 32 + col < p.n;
+        return in ? (y * 32 + row) * row_bytes + (x0 * 32 + col) * BYTES : kOutside;
+      };
+      if constexpr (VEC) {
 #pragma unroll
-      for (int y = 0; y < kPart; ++y)
+        for (int i = 0; i < kTimes; ++i) {
+          uint32_t from;
+          at[i] = place(i, from);
+          if constexpr (BYTES == 4) before[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(old, (int)at[i], 0, 0));
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kXs; ++x)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const f32x16& a = acc[x][y0 + y];
-          uint8_t* row = lds + (y * 32 + r) * kPitch;
+          const f32x16& a = acc[x0 + x][y];
           const uint32_t col = x * 32 + q * 8 + g * 4;
+          uint8_t* to = lds + r * kPitch + ((col / kElems) ^ (r & kMask)) * 16;
           if (BYTES == 2)
-            *reinterpret_cast<u32x2*>(row + (((col / 8) ^ (r & kMask)) * 16) + col % 8 * 2) = u32x2{bf16_pair(a[q * 4], a[q * 4 + 1]), bf16_pair(a[q * 4 + 2], a[q * 4 + 3])};
+            *reinterpret_cast<u32x2*>(to + col % 8 * 2) = u32x2{bf16_pair_here(a[q * 4], a[q * 4 + 1]), bf16_pair_here(a[q * 4 + 2], a[q * 4 + 3])};
           else
-            *reinterpret_cast<f32x4*>(row + (((col / 4) ^ (r & kMask)) * 16)) = f32x4{a[q * 4], a[q * 4 + 1], a[q * 4 + 2], a[q * 4 + 3]};
+            *reinterpret_cast<f32x4*>(to) = f32x4{a[q * 4], a[q * 4 + 1], a[q * 4 + 2], a[q * 4 + 3]};
         }
-    __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < kPart * 32 / kRowsAt; ++i) {
-      const uint32_t row = i * kRowsAt + lane / kPiecesRow, piece = lane % kPiecesRow;
-      const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + ((piece ^ (row & 31 & kMask)) * 16));
-      store_piece<BYTES>(p, m0 + y0 * 32 + row, n0 + piece * kElems, w);
+      for (int i = 0; i < kTimes; ++i) {
+        uint32_t from;
+        const uint32_t to = place(i, from);
+        if constexpr (VEC) {
+          u32x4 w = *reinterpret_cast<const u32x4*>(lds + from);
+          if constexpr (BYTES == 4) w = __builtin_bit_cast(u32x4, before[i] + __builtin_bit_cast(f32x4, w));
+          __builtin_amdgcn_raw_buffer_store_b128(w, c, (int)at[i], 0, 0);
+        } else if constexpr (BYTES == 2) {
+          __builtin_amdgcn_raw_buffer_store_b16(*reinterpret_cast<const uint16_t*>(lds + from), c, (int)to, 0, 0);
+        } else {
+          const float v = *reinterpret_cast<const float*>(lds + from) + __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(old, (int)to, 0, 0));
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), c, (int)to, 0, 0);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
-  }
 }
 
-// A tile of BM x BN of c per workgroup of WM * WN waves.  A step stages one 128-column block of BM rows of a and BN rows of
-// b in LDS (copied straight there, two buffers in turn), each row's eight 16-byte pieces at piece ^ row / 2 % 8: the
-// sixteen lanes that read at once, the same piece of sixteen rows, then meet all 64 banks.
-template <int BM, int BN, int WM, int WN, bool FAST>
+// Tiles of BM x BN of c, one after another per workgroup of WM * WN waves.  A step stages one 128-column block of BM rows of
+// a and BN rows of b in LDS (copied straight there, two buffers in turn), each row's eight 16-byte pieces at piece ^ row /
+// 2 % 8: the sixteen lanes that read at once, the same piece of sixteen rows, then meet all 64 banks.  The copies run two
+// blocks ahead of the products and through the ends of tiles: while a tile's results leave, the next one's first blocks
+// are on their way.  Every item has two blocks or more, or (ONE) a single one.
+template <int BM, int BN, int WM, int WN, int BYTES, bool VEC, bool FAST, bool ONE>
 __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs p) {
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kRows = BM + BN, kCopies = kRows / 8 / kWaves;
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && kRows % (8 * kWaves) == 0 && BM % (8 * kWaves) == 0, "tile");
-  __shared__ __align__(16) uint8_t lds[2][kRows * 128];
+  // two stages, and each wave's part for its results: one array, since between accesses to arrays that it can tell apart
+  // the compiler waits for the copies on their way
+  constexpr int kStage = kRows * 128;
+  __shared__ __align__(16) uint8_t lds[2 * kStage + kWaves * TN * 2048];
   const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  uint32_t tm, tn;
-  const uint32_t split = tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn);
-  const uint32_t m0 = tm * BM, n0 = tn * BN;
   const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
-  const Buffer abase = buffer_at(p.a.data + (int64_t)m0 * p.a.stride);
-  const Buffer bbase = buffer_at(p.b.data + (int64_t)n0 * p.b.stride);
+  const uint32_t items = p.tiles_m * p.tiles_n * p.splits;
 
-  // copies: rows [0, BM) of the stage are a's, the others b's; rows past the matrix read its last one
-  uint32_t from[kCopies];
+  // The copying side.  Rows [0, BM) of a stage are a's, the others b's.  What changes from tile to tile is the same for all
+  // lanes: where the tile's rows begin and how many bytes of them there are, and where their scale codes begin.  Rows
+  // past the matrix are beyond the buffer; scale codes past it are some other row's (a matrix's scales are a 128th of
+  // its data, below 2^32 bytes).
+  struct Source {
+    const uint8_t *a, *b;
+    uint32_t abytes, bbytes, acodes, bcodes, block, end;
+  };
+  auto source_of = [&](const Item& t) {
+    return Source{p.a.data + (int64_t)t.m0 * p.a.stride, p.b.data + (int64_t)t.n0 * p.b.stride,
+                  min(p.a.rows - t.m0, (uint32_t)BM) * (uint32_t)p.a.stride, min(p.b.rows - t.n0, (uint32_t)BN) * (uint32_t)p.b.stride,
+                  (t.m0 >> p.a.sh) * 4, (t.n0 >> p.b.sh) * 4, t.j0, t.j1};
+  };
+  Source source, upcoming;
+  uint32_t from[kCopies], acode[TM], bcode[TN];
 #pragma unroll
   for (int i = 0; i < kCopies; ++i) {
     const uint32_t row = (i * kWaves + wave) * 8 + lane / 8, piece = (lane % 8) ^ (row / 2 % 8);
-    if (i * kWaves * 8 < BM) from[i] = min(row, p.m - 1 - m0) * (uint32_t)p.a.stride + piece * 16;
-    else from[i] = min(row - BM, p.n - 1 - n0) * (uint32_t)p.b.stride + piece * 16;
+    from[i] = (i * kWaves * 8 < BM ? row * (uint32_t)p.a.stride : (row - BM) * (uint32_t)p.b.stride) + piece * 16;
   }
-  auto stage = [&](uint32_t j, uint8_t* to, int i) {
-    copy_to_lds(i * kWaves * 8 < BM ? abase : bbase, from[i], j * 128, to + (i * kWaves + wave) * 1024);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) acode[i] = 4 * ((wm + i * 32 + r) >> p.a.sh);
+#pragma unroll
+  for (int i = 0; i < TN; ++i) bcode[i] = 4 * ((wn + i * 32 + r) >> p.b.sh);
+  const Buffer ascales = buffer_at(p.a.scales, (p.kb + 3) / 4 * p.a.srows * 4), bscales = buffer_at(p.b.scales, (p.kb + 3) / 4 * p.b.srows * 4);
+  auto stage = [&](uint8_t* to, int i) {
+    copy_to_lds(i * kWaves * 8 < BM ? buffer_at(source.a, source.abytes) : buffer_at(source.b, source.bbytes), from[i], source.block * 128,
+                to + (i * kWaves + wave) * 1024);
   };
-
-  // scale codes of one block column for the lane's rows (a matrix's scales are a 128th of its data: below 2^32 bytes)
-  const Buffer ascales = buffer_at(p.a.scales), bscales = buffer_at(p.b.scales);
-  uint32_t acode[TM], bcode[TN];
-#pragma unroll
-  for (int t = 0; t < TM; ++t) acode[t] = 4 * (min(m0 + wm + t * 32 + r, p.m - 1) >> p.a.sh);
-#pragma unroll
-  for (int t = 0; t < TN; ++t) bcode[t] = 4 * (min(n0 + wn + t * 32 + r, p.n - 1) >> p.b.sh);
+  // to the next block, or the first one of the upcoming item
+  auto advance = [&] {
+    const bool same = ++source.block < source.end;
+    source.a = same ? source.a : upcoming.a;
+    source.b = same ? source.b : upcoming.b;
+    source.abytes = same ? source.abytes : upcoming.abytes;
+    source.bbytes = same ? source.bbytes : upcoming.bbytes;
+    source.acodes = same ? source.acodes : upcoming.acodes;
+    source.bcodes = same ? source.bcodes : upcoming.bcodes;
+    source.block = same ? source.block : upcoming.block;
+    source.end = same ? source.end : upcoming.end;
+  };
   struct Scales {
     int a[TM], b[TN];
   };
-  auto load_scales = [&](uint32_t j) {
+  auto load_scales = [&] {
+    const uint32_t aat = source.acodes + source.block / 4 * p.a.srows * 4 + source.block % 4;
+    const uint32_t bat = source.bcodes + source.block / 4 * p.b.srows * 4 + source.block % 4;
     Scales s;
 #pragma unroll
-    for (int t = 0; t < TM; ++t) s.a[t] = __builtin_amdgcn_raw_buffer_load_b8(ascales, (int)acode[t], (int)(j / 4 * p.a.srows * 4 + j % 4), 0);
+    for (int t = 0; t < TM; ++t) s.a[t] = __builtin_amdgcn_raw_buffer_load_b8(ascales, (int)acode[t], (int)aat, 0);
 #pragma unroll
-    for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)bcode[t], (int)(j / 4 * p.b.srows * 4 + j % 4), 0);
+    for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)bcode[t], (int)bat, 0);
     return s;
   };
 
@@ -416,7 +468,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
 
   // One half block: its matrix instructions, and spread evenly among them what `between(i)` does for i of kTiles.
   // Left alone the compiler would put all reads and copies behind them.
-  f32x16 acc[TN][TM] = {};
+  f32x16 acc[TN][TM];
   auto multiply = [&](const Codes& c, const Scales& s, auto between) {
     Bf16Codes ca[FAST ? 1 : TM], cb;
 #pragma unroll
@@ -437,19 +489,20 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
       }
   };
 
-  // Step j: block j's second half is read while its first is multiplied; then, once every wave has read all of block
-  // j and block j + 1 has landed, block j + 2 starts on its way into block j's buffer and the first half of block j + 1
-  // is read while the second of block j is multiplied.
+  // A step: the second half of the block in stage `in` is read while its first is multiplied; then, once every wave has read
+  // all of it and the next block has landed in the other buffer, the block after that starts on its way into stage `in` and
+  // the first half of the next one is read while the second half of this one is multiplied.
   Codes first;
   Scales now, next;
-  auto step = [&](uint32_t j, auto more, auto last) {
-    uint8_t *cur = lds[j & 1], *other = lds[(j + 1) & 1];
+  uint32_t in = 0;
+  auto step = [&] {
+    uint8_t *cur = lds + in * kStage, *other = lds + (in ^ 1) * kStage;
     Codes second;
     multiply(first, now, [&](int i) {
 #pragma unroll
       for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) second.piece[k] = read_piece(cur, 1, k);
     });
-    __syncthreads();
+    landed_barrier();
     __builtin_amdgcn_sched_barrier(0);
     // used from here on only: copied any earlier, they would be waited for there, and all copies with them
 #pragma unroll
@@ -457,50 +510,72 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
 #pragma unroll
     for (int t = 0; t < TN; ++t) asm volatile("" : "+v"(next.b[t]));
     const Scales landed = next;
-    if constexpr (decltype(more)::value) next = load_scales(j + 2);
+    advance();
+    next = load_scales();
     multiply(second, now, [&](int i) {
-      if constexpr (!decltype(last)::value) {
 #pragma unroll
-        for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) first.piece[k] = read_piece(other, 0, k);
-      }
-      if constexpr (decltype(more)::value) {
+      for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) first.piece[k] = read_piece(other, 0, k);
 #pragma unroll
-        for (int k = i * kCopies / kTiles; k < (i + 1) * kCopies / kTiles; ++k) stage(j + 2, cur, k);
-      }
+      for (int k = i * kCopies / kTiles; k < (i + 1) * kCopies / kTiles; ++k) stage(cur, k);
     });
     now = landed;
+    in ^= 1;
   };
-  const uint32_t j0 = (uint32_t)((uint64_t)p.kb * split / p.splits), j1 = (uint32_t)((uint64_t)p.kb * (split + 1) / p.splits);
-  if (j0 < j1) {
-    now = load_scales(j0);
-    next = load_scales(min(j0 + 1, j1 - 1));
+
+  Item t = item_of<BM, BN>(p, blockIdx.x);
+  source = upcoming = source_of(t);
+  if constexpr (!ONE) {
+    now = load_scales();
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) stage(j0, lds[j0 & 1], i);
-    __syncthreads();
-    if (j0 + 1 < j1) {
+    for (int i = 0; i < kCopies; ++i) stage(lds, i);
+    advance();
+    next = load_scales();
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) stage(j0 + 1, lds[(j0 + 1) & 1], i);
+    for (int i = 0; i < kCopies; ++i) stage(lds + kStage, i);
+    landed_barrier();
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds, 0, i);
+  }
+  for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
+#pragma unroll
+    for (int x = 0; x < TN; ++x)
+#pragma unroll
+      for (int y = 0; y < TM; ++y) acc[x][y] = f32x16{};
+    const Item done = t;
+    // behind the last item its own blocks are copied once more
+    if (b + gridDim.x < items) t = item_of<BM, BN>(p, b + gridDim.x);
+    upcoming = source_of(t);
+    if constexpr (ONE) {
+      __syncthreads();  // every wave has read the block before
+      now = load_scales();
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) stage(lds, i);
+      landed_barrier();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds, h, i);
+        multiply(first, now, [](int) {});
+      }
+      source = upcoming;
+    } else {
+      uint32_t j = done.j0;
+      do step();
+      while (++j < done.j1);
     }
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds[j0 & 1], 0, i);
-    for (uint32_t j = j0; j + 2 < j1; ++j) step(j, std::true_type{}, std::false_type{});
-    if (j0 + 1 < j1) step(j1 - 2, std::false_type{}, std::false_type{});
-    step(j1 - 1, std::false_type{}, std::true_type{});
+    // the results are read by instructions written out (bf16_pair_here), whose distance from the matrix instructions that
+    // write them, 19 wait states at most, the compiler does not keep by itself
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
+    // the lane as if it were new each time: addresses made from it and kept through the steps would not fit the registers
+    uint32_t me = lane;
+    asm volatile("" : "+v"(me));
+    ProductArgs out = p;
+    out.c = static_cast<uint8_t*>(p.c) + done.split * p.split_bytes;
+    store_turned<TM, TN, BYTES, VEC>(out, acc, lds + 2 * kStage + wave * TN * 2048, done.m0 + wm, done.n0 + wn, me);
   }
-  // Each wave turns its results in its own part of the LDS, so that they leave as whole rows of TN * 32 columns: 16-byte
-  // pieces, at piece ^ row % 32 of a row.
-  __syncthreads();
-  constexpr int kOut = BM * BN / kWaves;  // results of a wave
-  uint8_t* mine = lds[0] + wave * (sizeof(lds) / kWaves);
-  if (p.splits > 1) {
-    p.c = p.part + (int64_t)split * p.m * p.part_stride;
-    p.c_stride = p.part_stride;
-    p.c_vec = 1;
-    p.c_bf16 = p.accumulate = 0;
-  }
-  if (p.c_bf16) store_turned<TM, TN, 2>(p, acc, mine, m0 + wm, n0 + wn, lane);
-  else store_turned<TM, TN, 4>(p, acc, mine, m0 + wm, n0 + wn, lane);
-  static_assert(kOut * 2 <= (int)sizeof(lds) / kWaves, "a wave's bf16 results fit its part");
+  landed_barrier();  // no copy is on its way any more when the LDS goes to another workgroup
 }
 
 // c from the sums of the splits, in their order; a lane takes four columns.
@@ -516,15 +591,46 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs p) {
   }
 }
 
-template <int BM, int BN, int WM, int WN>
-void launch_tile(ProductArgs a, bool fast, hipStream_t st) {
+template <int BM, int BN, int BYTES, bool VEC, bool ONE>
+void launch_tiles(ProductArgs a, bool fast, hipStream_t st) {
   a.tiles_m = (uint32_t)ceil_div(a.m, BM);
   a.tiles_n = (uint32_t)ceil_div(a.n, BN);
-  const dim3 grid(a.tiles_m * a.tiles_n * a.splits), block(64 * WM * WN);
-  if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((product_tile_kernel<BM, BN, WM, WN, false>), grid, block, 0, st, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL(join_splits_kernel, dim3((uint32_t)std::min<int64_t>(2048, ceil_div(a.m * (a.part_stride / 4), 256))), dim3(256), 0, st, a);
+  // as many workgroups as the LDS of 256 CUs holds; a multiple of the XCDs keeps a workgroup's items on its XCD
+  constexpr uint32_t kResident = 256 * (160 / ((BM + BN) / 4 + BN / 8));
+  const dim3 grid(std::min(a.tiles_m * a.tiles_n * a.splits, kResident)), block(256);
+  if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, true, ONE>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, false, ONE>), grid, block, 0, st, a);
+}
+
+// Tiles of 256 want rows of whole 16-byte pieces and two blocks or more.
+template <int BYTES>
+void launch_tile_kind(const ProductArgs& a, bool large, bool fast, hipStream_t st) {
+  if (a.kb == 1) {
+    if (a.c_vec) launch_tiles<128, 128, BYTES, true, true>(a, fast, st);
+    else launch_tiles<128, 128, BYTES, false, true>(a, fast, st);
+  } else if (a.c_vec) {
+    if (large) launch_tiles<256, 256, BYTES, true, false>(a, fast, st);
+    else launch_tiles<128, 128, BYTES, true, false>(a, fast, st);
+  } else {
+    launch_tiles<128, 128, BYTES, false, false>(a, fast, st);
+  }
+}
+
+void launch_tile(const ProductArgs& a, bool large, bool fast, hipStream_t st) {
+  if (a.splits == 1) {
+    if (a.c_bf16) launch_tile_kind<2>(a, large, fast, st);
+    else launch_tile_kind<4>(a, large, fast, st);
+    return;
+  }
+  ProductArgs parts = a;
+  parts.c = a.part;
+  parts.c_stride = a.part_stride;
+  parts.split_bytes = (int64_t)a.m * a.part_stride * (int64_t)sizeof(float);
+  parts.c_vec = 1;
+  parts.n = (uint32_t)a.part_stride;  // columns past b's last one: sums of zeros
+  parts.accumulate = 0;
+  launch_tile_kind<4>(parts, large, fast, st);
+  hipLaunchKernelGGL(join_splits_kernel, dim3((uint32_t)std::min<int64_t>(2048, ceil_div(a.m * (a.part_stride / 4), 256))), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -540,7 +646,8 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   a.m = l.m;
   a.n = l.n;
   a.kb = l.kb;
-  a.c_vec = reinterpret_cast<uintptr_t>(l.c) % 16 == 0 && l.c_stride * (l.c_bf16 ? 2 : 4) % 16 == 0;
+  const int size = l.c_bf16 ? 2 : 4;
+  a.c_vec = reinterpret_cast<uintptr_t>(l.c) % 16 == 0 && l.c_stride * size % 16 == 0;
   a.c_bf16 = l.c_bf16;
   a.accumulate = l.accumulate;
   if (l.x) {
@@ -553,12 +660,13 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
       if (vec) launch_few_rows<1, kF32 | kVec>(a, l.fast, st);
       else launch_direct<1, 1, 8, kF32>(a, l.fast, st);
     }
-  } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect) {
+  } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect && l.c_stride * size < 1 << 24) {
     a.splits = plan.splits;
+    a.split_bytes = 0;
+    if (l.n * (int64_t)size % 16) a.c_vec = 0;  // whole pieces only
     a.part = static_cast<float*>(l.workspace);
     a.part_stride = part_stride(l.n);
-    if (plan.kind == ProductPlan::kTile256) launch_tile<256, 256, 2, 2>(a, l.fast, st);
-    else launch_tile<128, 128, 2, 2>(a, l.fast, st);
+    launch_tile(a, plan.kind == ProductPlan::kTile256, l.fast, st);
   } else {
     if (l.m <= 16) launch_few_rows<1, kCodes>(a, l.fast, st);
     else launch_few_rows<2, kCodes>(a, l.fast, st);

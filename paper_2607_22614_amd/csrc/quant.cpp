@@ -125,7 +125,7 @@ int check_workspace(const void* p, uint64_t have, uint64_t need, const char* wha
 // tile alone on its CU 0.63 (0.78) and of two of them together 0.96 (1.72); what a tile costs beside its steps 8 and 1.5;
 // a launch 4; joining splits 2.5 and their sums' bytes, written and read, at 6.5 TB/s.
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
-  if (m <= 32) return {ProductPlan::kDirect, 1};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
+  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.63 : 0.78, pair128 = fast ? 0.96 : 1.72;
   ProductPlan best{ProductPlan::kTile256, 1};

@@ -201,6 +201,27 @@ def test_linear(m, n, k, dtype):
         _close(y, want, size, k, out_type == torch.bfloat16)
 
 
+@pytest.mark.parametrize("m,n,k", [(4100, 4360, 256), (4100, 4360, 300), (4352, 4096, 520), (3000, 3001, 256), (3001, 2999, 384), (5000, 2600, 1030),
+                                   (8200, 2050, 100), (8200, 2051, 128), (300, 16400, 640), (40, 70000, 300)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_more_tiles_than_workgroups(m, n, k, fast):
+    """Workgroups that go from tile to tile, of two blocks and more and of a single one, at the edges of c and inside."""
+    dr = _dr()
+    a, av = _matrix(dr, m, k, 1, m + k, spread=3)
+    b, bv = _matrix(dr, n, k, 128, n + k, spread=3)
+    av, bv = torch.from_numpy(av).cuda(), torch.from_numpy(bv).cuda()
+    want, size = av @ bv.t(), av.abs() @ bv.abs().t()
+    n_sum = -(-k // 128) * 128 + 64
+    tol = (n_sum * 2.0**-23 + (2.0**-10 if fast else 0)) * size
+    ws = _workspace(dr, m, n, k)
+    for dtype, accumulate in ((torch.bfloat16, False), (torch.float32, False), (torch.float32, True)):
+        say("many tiles", m, n, k, fast, dtype, accumulate)
+        out = torch.full((m, n), 3.0, dtype=dtype, device="cuda")
+        dr.dr_qmatmul(a, b, out, accumulate=accumulate, fast=fast, workspace=ws)
+        off = (out.to(torch.float64) - want - (3.0 if accumulate else 0.0)).abs()
+        assert (off <= tol + (want.abs() * 2.0**-8 if dtype == torch.bfloat16 else 2.0**-20)).all()
+
+
 @pytest.mark.parametrize("m", [1, 16, 20, 32])
 @pytest.mark.parametrize("n,k", [(4097, 264), (16385, 130), (20001, 1160)])
 @pytest.mark.parametrize("fast", [False, True])

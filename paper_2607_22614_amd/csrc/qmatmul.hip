@@ -86,9 +86,10 @@ __device__ __forceinline__ void store4(const ProductArgs& p, uint32_t m, uint32_
   }
 }
 
-// A lane's 32 elements of 128 columns of one row of x, as they lie in memory.  How x comes: fp32 or bf16, in rows of whole
-// 16-byte pieces (kVec: loads without branches, which the compiler leaves in flight) or any rows; or as codes.
-enum XKind { kCodes = 0, kF32 = 1, kBf16 = 2, kVec = 4 };
+// How x comes: as codes, or as rows of fp32 or bf16 (kShort: of fewer than 8 elements).
+enum XKind { kCodes = 0, kF32 = 1, kBf16 = 2, kShort = 4 };
+
+// A lane's 32 elements of 128 columns of one row of x, as load_row8 gives them.
 template <int X>
 struct Elements {
   Raw8<(X & kBf16) != 0> v[X == kCodes ? 1 : 4];
@@ -101,25 +102,9 @@ __device__ __forceinline__ Elements<X> load_elements(const ProductArgs& p, uint3
   for (int q = 0; q < 4; ++q) {
     const uint32_t c = col + (q >> 1) * 64 + (q & 1) * 8;
     const int64_t at = (int64_t)row * p.x_stride;
-    if (X & kVec) {
-      const u32x4* x = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.x) + (at + min(c, p.a.cols - 8)) * (BF16 ? 2 : 4));
-#pragma unroll
-      for (int i = 0; i < (BF16 ? 1 : 2); ++i) e.v[q].w[i] = x[i];
-    } else {
-      e.v[q] = load_raw8<BF16>(p.x, at + c, max(0, min(8, (int)p.a.cols - (int)c)), false);
-    }
+    e.v[q] = X & kShort ? load_short_row8<BF16>(p.x, at, c, p.a.cols) : load_row8<BF16>(p.x, at, c, p.a.cols);
   }
   return e;
-}
-// Zeros in place of what kVec loads read again from columns that are not there (pieces are all there or not at all).
-template <int X>
-__device__ __forceinline__ void clear_beyond(const ProductArgs& p, uint32_t col, Elements<X>& e) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int i = 0; i < ((X & kBf16) ? 1 : 2); ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) e.v[q].w[i][w] = col + (q >> 1) * 64 + (q & 1) * 8 < p.a.cols ? e.v[q].w[i][w] : 0u;
 }
 
 // Their codes, and the scale of the row's 128 columns, as dr_quantize gives them.
@@ -196,7 +181,10 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       if constexpr (X != 0) {
-        if ((X & kVec) && j * 128 + 128 > p.a.cols) clear_beyond<X>(p, j * 128 + g * 16, k.x[t]);
+        if (!(X & kShort) && j * 128 + 128 > p.a.cols) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) settle8(k.x[t].v[q], j * 128 + g * 16 + (q >> 1) * 64 + (q & 1) * 8, p.a.cols);
+        }
         aw[t] = quantize_block(k.x[t], k.ea[t]);
       } else {
         aw[t] = k.a[t];
@@ -651,14 +639,13 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   a.c_bf16 = l.c_bf16;
   a.accumulate = l.accumulate;
   if (l.x) {
-    // rows that are no whole 16-byte pieces are loaded element by element, by one form of the kernel
-    const bool vec = l.x_aligned && l.a.cols % 8 == 0;
+    const bool shorter = l.a.cols < 8;
     if (l.x_bf16) {
-      if (vec) launch_few_rows<1, kBf16 | kVec>(a, l.fast, st);
-      else launch_direct<1, 1, 8, kBf16>(a, l.fast, st);
+      if (shorter) launch_direct<1, 1, 8, kBf16 | kShort>(a, l.fast, st);
+      else launch_few_rows<1, kBf16>(a, l.fast, st);
     } else {
-      if (vec) launch_few_rows<1, kF32 | kVec>(a, l.fast, st);
-      else launch_direct<1, 1, 8, kF32>(a, l.fast, st);
+      if (shorter) launch_direct<1, 1, 8, kF32 | kShort>(a, l.fast, st);
+      else launch_few_rows<1, kF32>(a, l.fast, st);
     }
   } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect && l.c_stride * size < 1 << 24) {
     a.splits = plan.splits;

@@ -61,10 +61,6 @@ int check_results(int64_t m, int64_t n, const char* what) {
   return m * n <= 1ll << 38 ? DR_OK : fail(DR_EINVAL, "%s: %lld x %lld results (at most 2^38)", what, (long long)m, (long long)n);
 }
 
-bool aligned_rows(const void* p, int64_t row_stride, int32_t type) {
-  return aligned(p, 16) && row_stride * element_bytes(type) % 16 == 0;
-}
-
 int hip_result(hipError_t e, const char* what) {
   return e == hipSuccess ? DR_OK : fail(DR_EHIP, "%s: kernel launch: %s", what, hipGetErrorString(e));
 }
@@ -81,7 +77,6 @@ int quantize(const void* src, int32_t type, int64_t rows, int64_t cols, int64_t 
   l.rows = (uint32_t)rows;
   l.cols = (uint32_t)cols;
   l.bf16 = type == DR_TYPE_BF16;
-  l.aligned = aligned_rows(src, row_stride, type);
   if (q) l.q = view(*q);
   if (qt) l.qt = view(*qt);
   return hip_result(launch_quantize(l, st), what);
@@ -262,7 +257,6 @@ extern "C" int dr_qlinear(const void* x, int32_t x_type, int64_t m, int64_t x_ro
     l.x = x;
     l.x_stride = x_row_stride;
     l.x_bf16 = x_type == DR_TYPE_BF16;
-    l.x_aligned = aligned_rows(x, x_row_stride, x_type);
     l.a.cols = (uint32_t)k;
   } else {
     uint8_t* ws = static_cast<uint8_t*>(workspace);

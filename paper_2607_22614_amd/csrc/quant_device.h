@@ -1,4 +1,4 @@
-// Device helpers of the 8-bit and gradient kernels: scales, rounding to e4m3, loads and stores of 8 elements.
+// Device helpers of the 8-bit and gradient kernels: scales, rounding to e4m3, loads of 8 elements.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -47,31 +47,56 @@ struct Raw8 {
   u32x4 w[BF16 ? 1 : 2];
 };
 
-// Elements [0, n) of the 8 at `at`, n <= 8; the others are 0.  vec: 16-byte loads where all 8 are there.
+// 16 bytes at any element: the memory takes that
 template <bool BF16>
-__device__ __forceinline__ Raw8<BF16> load_raw8(const void* base, int64_t at, int n, bool vec) {
+struct AnyElement {
+  typedef u32x4 __attribute__((aligned(4))) type;
+};
+template <>
+struct AnyElement<true> {
+  typedef u32x4 __attribute__((aligned(2))) type;
+};
+
+// Elements col .. col + 7 of the row of `cols` elements at element `row` of base, aligned to the element alone.  The last 8
+// of the row stand in for those that are not all there, so that every lane loads and none branches; settle8 puts that
+// right.  A row of fewer than 8 is loaded element by element, and is right at once.
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> load_row8(const void* base, int64_t row, uint32_t col, uint32_t cols) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + (row + min(col, cols - 8)) * (BF16 ? 2 : 4);
+  Raw8<BF16> v;
+#pragma unroll
+  for (int i = 0; i < (BF16 ? 1 : 2); ++i) v.w[i] = reinterpret_cast<const typename AnyElement<BF16>::type*>(p)[i];
+  return v;
+}
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> load_short_row8(const void* base, int64_t row, uint32_t col, uint32_t cols) {
   Raw8<BF16> v = {};
-  if (BF16) {
-    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-    if (vec && n >= 8) {
-      v.w[0] = *reinterpret_cast<const u32x4*>(p);
-    } else if (n > 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) v.w[0][i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
-    }
-  } else {
-    const uint32_t* p = static_cast<const uint32_t*>(base) + at;
-    if (vec && n >= 8) {
-      v.w[0] = *reinterpret_cast<const u32x4*>(p);
-      v.w[BF16 ? 0 : 1] = *reinterpret_cast<const u32x4*>(p + 4);
-    } else if (n > 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) v.w[BF16 ? 0 : i / 4][i % 4] = p[i];
-    }
+  for (uint32_t i = 0; i < 7; ++i) {
+    if (BF16) v.w[0][i / 2] |= col + i < cols ? (uint32_t)static_cast<const uint16_t*>(base)[row + i] << (i % 2 * 16) : 0u;
+    else v.w[BF16 ? 0 : i / 4][i % 4] = col + i < cols ? static_cast<const uint32_t*>(base)[row + i] : 0u;
   }
   return v;
+}
+// What load_row8 gave, with the elements that are there in their places and zeros behind them.
+template <bool BF16>
+__device__ __forceinline__ void settle8(Raw8<BF16>& v, uint32_t col, uint32_t cols) {
+  const uint32_t s = col - min(col, cols - 8);  // elements too many in front
+  if (!__any(s)) return;
+  constexpr int kWords = BF16 ? 4 : 8, kPer = 8 / kWords;  // elements in a word
+  uint32_t w[kWords];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) w[i] = s < 8 ? v.w[i / 4][i % 4] : 0u;
+#pragma unroll
+  for (int d = kWords / 2; d; d /= 2)
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = s & (d * kPer) ? (i + d < kWords ? w[i + d] : 0u) : w[i];
+  if (BF16) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = s & 1 ? w[i] >> 16 | (i + 1 < kWords ? w[i + 1] << 16 : 0u) : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) v.w[i / 4][i % 4] = w[i];
 }
 
 // fp32 bits of element i.
@@ -159,43 +184,9 @@ __device__ __forceinline__ u32x2 column_codes(const Raw8<BF16> (&v)[8], int j, u
   return r;
 }
 
-// The same as fp32.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t at, int n, bool vec, float (&v)[8]) {
-  const Raw8<BF16> w = load_raw8<BF16>(base, at, n, vec);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(bits_of<BF16>(w, i));
-}
-
 // fp32 -> bf16, ties to even (the hardware convert).
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
-}
-
-// Elements [0, n) of v to the 8 at `at`, n <= 8.  vec: 16-byte stores where all 8 are there.
-template <bool BF16>
-__device__ __forceinline__ void store8(void* base, int64_t at, int n, bool vec, const float (&v)[8]) {
-  if (BF16) {
-    uint16_t* p = static_cast<uint16_t*>(base) + at;
-    const u32x4 w = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-    if (vec && n >= 8) {
-      *reinterpret_cast<u32x4*>(p) = w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
-    }
-  } else {
-    float* p = static_cast<float*>(base) + at;
-    if (vec && n >= 8) {
-      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = v[i];
-    }
-  }
 }
 
 }  // namespace dr

@@ -30,7 +30,7 @@ struct QuantizeLaunch {
   const void* src;
   int64_t src_stride;  // elements
   uint32_t rows, cols;
-  bool bf16, aligned;  // aligned: 16-byte aligned rows
+  bool bf16;
   QView q, qt;         // data null: not wanted
 };
 hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st);
@@ -40,7 +40,7 @@ struct ProductLaunch {
   QView a, b;
   const void* x;     // set: a is quantized in the kernel from these rows
   int64_t x_stride;  // elements
-  bool x_bf16, x_aligned;
+  bool x_bf16;
   void* c;
   int64_t c_stride;  // elements
   uint32_t m, n, kb;

@@ -16,9 +16,18 @@ struct QuantizeArgs {
   const void* src;
   int64_t src_stride;
   uint32_t rows, cols, tiles_x;
-  int32_t vec;
   QView q, qt;
 };
+
+// Eight columns of ROWS rows; rows past the matrix read its last one.
+template <bool BF16, int ROWS>
+__device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, uint32_t col, Raw8<BF16> (&v)[ROWS]) {
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int64_t row = (int64_t)min(row0 + i, a.rows - 1) * a.src_stride;
+    v[i] = a.cols >= 8 ? load_row8<BF16>(a.src, row, col, a.cols) : load_short_row8<BF16>(a.src, row, col, a.cols);
+  }
+}
 
 // Blocks of 1 x 128, rows only.  A wave takes 512 columns (four blocks, 16 lanes each, 8 elements a lane) of
 // ROWS rows, whose loads are all in flight together; a block's maximum is a DPP reduction over its 16
@@ -32,10 +41,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void quantize_rows_kernel(QuantizeA
   const uint32_t row0 = (blockIdx.x / a.tiles_x * kRowWaves + wave) * ROWS;
   if (row0 >= a.rows) return;
   const uint32_t col = quad * 512 + lane * 8;
-  const int n = max(0, min(8, (int)a.cols - (int)col));
   Raw8<BF16> v[ROWS];
+  load_rows(a, row0, col, v);
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) v[i] = load_raw8<BF16>(a.src, (int64_t)min(row0 + i, a.rows - 1) * a.src_stride + col, n, a.vec);
+  for (int i = 0; i < ROWS; ++i)
+    if (a.cols >= 8) settle8(v[i], col, a.cols);
   uint32_t word = 0;
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
@@ -73,12 +83,12 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;
   const uint32_t ct = blockIdx.x % a.tiles_x, rt = blockIdx.x / a.tiles_x;
   const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * 8;
-  const int n = max(0, min(8, (int)a.cols - (int)col));
   Raw8<BF16> v[8];
+  load_rows(a, row0, col, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const bool in = row0 + i < a.rows;
-    v[i] = load_raw8<BF16>(a.src, (int64_t)(in ? row0 + i : a.rows - 1) * a.src_stride + col, in ? n : 0, a.vec);
+    if (a.cols >= 8) settle8(v[i], col, a.cols);
+    if (row0 + i >= a.rows) v[i] = Raw8<BF16>{};
   }
   // the lane's largest magnitude of each row; finite ones only if any is not
   uint32_t rmax[8], top = 0;
@@ -190,7 +200,6 @@ hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
   a.src_stride = l.src_stride;
   a.rows = l.rows;
   a.cols = l.cols;
-  a.vec = l.aligned;
   a.q = l.q;
   a.qt = l.qt;
   const bool square = (l.q.data ? l.q.sh : l.qt.sh) != 0;

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
       if constexpr (X != 0) {
         if (!(X & kShort) && j * 128 + 128 > p.a.cols) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) settle8(k.x[t].v[q], j * 128 + g * 16 + (q >> 1) * 64 + (q & 1) * 8, p.a.cols);
+          for (int q = 0; q < 4; ++q) settle8(k.x[t].v[q], ahead8(j * 128 + g * 16 + (q >> 1) * 64 + (q & 1) * 8, p.a.cols));
         }
         aw[t] = quantize_block(k.x[t], k.ea[t]);
       } else {

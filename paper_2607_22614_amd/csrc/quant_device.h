@@ -78,11 +78,11 @@ __device__ __forceinline__ Raw8<BF16> load_short_row8(const void* base, int64_t 
   }
   return v;
 }
-// What load_row8 gave, with the elements that are there in their places and zeros behind them.
+// Elements too many in front of those that load_row8 was asked for; 0 in a row of fewer than 8.
+__device__ __forceinline__ uint32_t ahead8(uint32_t col, uint32_t cols) { return cols < 8 ? 0 : col - min(col, cols - 8); }
+// What load_row8 gave, with s elements too many in front: the elements that are there in their places, zeros behind them.
 template <bool BF16>
-__device__ __forceinline__ void settle8(Raw8<BF16>& v, uint32_t col, uint32_t cols) {
-  const uint32_t s = col - min(col, cols - 8);  // elements too many in front
-  if (!__any(s)) return;
+__device__ __forceinline__ void settle8(Raw8<BF16>& v, uint32_t s) {
   constexpr int kWords = BF16 ? 4 : 8, kPer = 8 / kWords;  // elements in a word
   uint32_t w[kWords];
 #pragma unroll

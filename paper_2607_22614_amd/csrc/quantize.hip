@@ -27,6 +27,11 @@ __device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, 
     const int64_t row = (int64_t)min(row0 + i, a.rows - 1) * a.src_stride;
     v[i] = a.cols >= 8 ? load_row8<BF16>(a.src, row, col, a.cols) : load_short_row8<BF16>(a.src, row, col, a.cols);
   }
+  const uint32_t s = ahead8(col, a.cols);
+  if (__any(s)) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) settle8(v[i], s);
+  }
 }
 
 // Blocks of 1 x 128, rows only.  A wave takes 512 columns (four blocks, 16 lanes each, 8 elements a lane) of
@@ -43,9 +48,6 @@ __global__ __launch_bounds__(64 * kRowWaves) void quantize_rows_kernel(QuantizeA
   const uint32_t col = quad * 512 + lane * 8;
   Raw8<BF16> v[ROWS];
   load_rows(a, row0, col, v);
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i)
-    if (a.cols >= 8) settle8(v[i], col, a.cols);
   uint32_t word = 0;
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
@@ -85,10 +87,10 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * 8;
   Raw8<BF16> v[8];
   load_rows(a, row0, col, v);
+  if (row0 + 8 > a.rows) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (a.cols >= 8) settle8(v[i], col, a.cols);
-    if (row0 + i >= a.rows) v[i] = Raw8<BF16>{};
+    for (int i = 0; i < 8; ++i)
+      if (row0 + i >= a.rows) v[i] = Raw8<BF16>{};
   }
   // the lane's largest magnitude of each row; finite ones only if any is not
   uint32_t rmax[8], top = 0;

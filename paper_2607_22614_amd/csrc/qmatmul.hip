@@ -306,7 +306,7 @@ constexpr uint32_t kOutside = 1u << 31;  // 128 rows of c lie within it (launch_
 template <int TM, int TN, int BYTES, bool VEC>
 __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 (&acc)[TN][TM], uint8_t* lds, uint32_t m0, uint32_t n0, uint32_t lane) {
   constexpr int kXs = TN * 2 / BYTES, kPitch = TN * 64, kPiecesRow = kPitch / 16, kMask = kPiecesRow - 1, kElems = 16 / BYTES;
-  constexpr int kSize = VEC ? 16 : BYTES, kAcross = kPitch / kSize, kRowsAt = kAcross < 64 ? 64 / kAcross : 1, kTimes = 32 * kPitch / kSize / 64;
+  constexpr int kSize = VEC ? 16 : BYTES, kAcross = kPitch / kSize, kTimes = 32 * kPitch / kSize / 64;
   static_assert((kPiecesRow & kMask) == 0 && kXs * 32 * BYTES == kPitch, "rows of a power of two of pieces");
   const uint32_t r = lane & 31, g = lane >> 5, row_bytes = (uint32_t)p.c_stride * BYTES;
   const uint8_t* base = static_cast<const uint8_t*>(p.c) + ((int64_t)m0 * p.c_stride + n0) * BYTES;

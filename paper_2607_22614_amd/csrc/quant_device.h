@@ -60,12 +60,16 @@ struct AnyElement<true> {
 // Elements col .. col + 7 of the row of `cols` elements at element `row` of base, aligned to the element alone.  The last 8
 // of the row stand in for those that are not all there, so that every lane loads and none branches; settle8 puts that
 // right.  A row of fewer than 8 is loaded element by element, and is right at once.
-template <bool BF16>
+// STREAM: rows that begin at whole 16 bytes and are read once.
+template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ Raw8<BF16> load_row8(const void* base, int64_t row, uint32_t col, uint32_t cols) {
   const uint8_t* p = static_cast<const uint8_t*>(base) + (row + min(col, cols - 8)) * (BF16 ? 2 : 4);
   Raw8<BF16> v;
 #pragma unroll
-  for (int i = 0; i < (BF16 ? 1 : 2); ++i) v.w[i] = reinterpret_cast<const typename AnyElement<BF16>::type*>(p)[i];
+  for (int i = 0; i < (BF16 ? 1 : 2); ++i) {
+    if constexpr (STREAM) v.w[i] = load_stream(reinterpret_cast<const u32x4*>(p) + i);
+    else v.w[i] = reinterpret_cast<const typename AnyElement<BF16>::type*>(p)[i];
+  }
   return v;
 }
 template <bool BF16>
@@ -142,15 +146,17 @@ __device__ __forceinline__ uint32_t row_max(const Raw8<BF16>& v, bool finite) {
 }
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
+// What two converts overwrite, one half each: no instruction sets it.
+__device__ __forceinline__ s16x2 any_halves() { return __builtin_nondeterministic_value(s16x2{}); }
 // Four values over the scale as e4m3 codes: the hardware converts divide by the power of two exactly, round to even and
 // make NaN of what is not finite.  Values are within 448 after scaling.
 __device__ __forceinline__ uint32_t to_e4m3_f32(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {
-  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, __uint_as_float(a), __uint_as_float(b), scale, false);
+  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(any_halves(), __uint_as_float(a), __uint_as_float(b), scale, false);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __uint_as_float(c), __uint_as_float(d), scale, true);
   return __builtin_bit_cast(uint32_t, w);
 }
 __device__ __forceinline__ uint32_t to_e4m3_bf16(uint32_t ab, uint32_t cd, float scale) {
-  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, ab), scale, false);
+  s16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(any_halves(), __builtin_bit_cast(bf16x2, ab), scale, false);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, cd), scale, true);
   return __builtin_bit_cast(uint32_t, w);
 }

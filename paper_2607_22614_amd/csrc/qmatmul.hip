@@ -23,6 +23,7 @@ struct ProductArgs {
   void* c;
   int64_t c_stride;
   uint32_t m, n, kb, tiles_m, tiles_n;
+  uint32_t first, count, quarters;  // the tiles of the launch, and whether an item is a quarter of one (item_of)
   uint32_t splits;  // of the blocks: items of one tile, whose fp32 sums go to part[split][m][part_stride]
   int64_t split_bytes;  // of c, from one split to the next (0 without them)
   int32_t c_vec, c_bf16, accumulate;
@@ -272,20 +273,24 @@ __device__ __forceinline__ void landed_barrier() {
   __syncthreads();
 }
 
-// Work item b of a product: the tile at (m0, n0) and its blocks [j0, j1), one split's.  Each XCD takes a contiguous eighth
+// Work item b of a product: a tile (m0, n0) and its blocks [j0, j1), one split's.  Each XCD takes a contiguous eighth
 // of the items; the tiles of a split follow one another in bands of kBand tiles down, so that the workgroups running at
-// once on an XCD share rows of both operands in its L2.
+// once on an XCD share rows of both operands in its L2.  A launch takes `count` tiles from `first` on, in this order; or,
+// as `quarters`, the four BM x BN parts of each of that many tiles of twice the size, which may lie outside of c.
 constexpr uint32_t kBand = 8;
 struct Item {
   uint32_t m0, n0, split, j0, j1;
 };
 __device__ __forceinline__ uint32_t same(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint32_t items_of(const ProductArgs& p) { return p.count * p.splits << 2 * p.quarters; }
 template <int BM, int BN>
 __device__ __forceinline__ Item item_of(const ProductArgs& p, uint32_t b) {
-  const uint32_t tiles = p.tiles_m * p.tiles_n, all = xcd_tile(b, tiles * p.splits), split = all / tiles, t = all % tiles;
+  const uint32_t at = xcd_tile(b, items_of(p)), part = at & (p.quarters * 3), all = at >> 2 * p.quarters;
+  const uint32_t split = all / p.count, t = p.first + all % p.count;
   const uint32_t band = t / (kBand * p.tiles_n), high = min(kBand, p.tiles_m - band * kBand), i = t - band * kBand * p.tiles_n;
+  const uint32_t y = (band * kBand + i % high << p.quarters) + part % 2, x = (i / high << p.quarters) + part / 2;
   // the same for the whole workgroup, which the compiler does not see behind the divisions
-  return Item{same((band * kBand + i % high) * BM), same(i / high * BN), same(split), same((uint32_t)((uint64_t)p.kb * split / p.splits)),
+  return Item{same(y * BM), same(x * BN), same(split), same((uint32_t)((uint64_t)p.kb * split / p.splits)),
               same((uint32_t)((uint64_t)p.kb * (split + 1) / p.splits))};
 }
 
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
-  const uint32_t items = p.tiles_m * p.tiles_n * p.splits;
+  const uint32_t items = items_of(p);
 
   // The copying side.  Rows [0, BM) of a stage are a's, the others b's.  What changes from tile to tile is the same for all
   // lanes: where the tile's rows begin and how many bytes of them there are, and where their scale codes begin.  Rows
@@ -393,7 +398,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   };
   auto source_of = [&](const Item& t) {
     return Source{p.a.data + (int64_t)t.m0 * p.a.stride, p.b.data + (int64_t)t.n0 * p.b.stride,
-                  min(p.a.rows - t.m0, (uint32_t)BM) * (uint32_t)p.a.stride, min(p.b.rows - t.n0, (uint32_t)BN) * (uint32_t)p.b.stride,
+                  (min(t.m0 + BM, p.a.rows) - min(t.m0, p.a.rows)) * (uint32_t)p.a.stride,
+                  (min(t.n0 + BN, p.b.rows) - min(t.n0, p.b.rows)) * (uint32_t)p.b.stride,
                   (t.m0 >> p.a.sh) * 4, (t.n0 >> p.b.sh) * 4, t.j0, t.j1};
   };
   Source source, upcoming;
@@ -580,34 +586,49 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs p) {
 }
 
 template <int BM, int BN, int BYTES, bool VEC, bool ONE>
-void launch_tiles(ProductArgs a, bool fast, hipStream_t st) {
-  a.tiles_m = (uint32_t)ceil_div(a.m, BM);
-  a.tiles_n = (uint32_t)ceil_div(a.n, BN);
+void launch_items(const ProductArgs& a, bool fast, hipStream_t st) {
   // as many workgroups as the LDS of 256 CUs holds; a multiple of the XCDs keeps a workgroup's items on its XCD
   constexpr uint32_t kResident = 256 * (160 / ((BM + BN) / 4 + BN / 8));
-  const dim3 grid(std::min(a.tiles_m * a.tiles_n * a.splits, kResident)), block(256);
+  const dim3 grid(std::min(a.count * a.splits << 2 * a.quarters, kResident)), block(256);
   if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, true, ONE>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, false, ONE>), grid, block, 0, st, a);
 }
 
-// Tiles of 256 want rows of whole 16-byte pieces and two blocks or more.
-template <int BYTES>
-void launch_tile_kind(const ProductArgs& a, bool large, bool fast, hipStream_t st) {
-  if (a.kb == 1) {
-    if (a.c_vec) launch_tiles<128, 128, BYTES, true, true>(a, fast, st);
-    else launch_tiles<128, 128, BYTES, false, true>(a, fast, st);
-  } else if (a.c_vec) {
-    if (large) launch_tiles<256, 256, BYTES, true, false>(a, fast, st);
-    else launch_tiles<128, 128, BYTES, true, false>(a, fast, st);
-  } else {
-    launch_tiles<128, 128, BYTES, false, false>(a, fast, st);
+// All tiles but the last `quartered` ones of 256 x 256, and these as tiles of 128 x 128 in a second launch.
+template <int BM, int BN, int BYTES, bool VEC, bool ONE>
+void launch_tiles(ProductArgs a, uint32_t quartered, bool fast, hipStream_t st) {
+  a.tiles_m = (uint32_t)ceil_div(a.m, BM);
+  a.tiles_n = (uint32_t)ceil_div(a.n, BN);
+  a.first = a.quarters = 0;
+  a.count = a.tiles_m * a.tiles_n - quartered;
+  launch_items<BM, BN, BYTES, VEC, ONE>(a, fast, st);
+  if constexpr (BM == 256 && BN == 256) {
+    if (!quartered) return;
+    a.first = a.count;
+    a.count = quartered;
+    a.quarters = 1;
+    launch_items<128, 128, BYTES, VEC, ONE>(a, fast, st);
   }
 }
 
-void launch_tile(const ProductArgs& a, bool large, bool fast, hipStream_t st) {
+// Tiles of 256 want rows of whole 16-byte pieces and two blocks or more.
+template <int BYTES>
+void launch_tile_kind(const ProductArgs& a, const ProductPlan& plan, bool fast, hipStream_t st) {
+  if (a.kb == 1) {
+    if (a.c_vec) launch_tiles<128, 128, BYTES, true, true>(a, 0, fast, st);
+    else launch_tiles<128, 128, BYTES, false, true>(a, 0, fast, st);
+  } else if (a.c_vec) {
+    if (plan.kind == ProductPlan::kTile256) launch_tiles<256, 256, BYTES, true, false>(a, plan.quartered, fast, st);
+    else launch_tiles<128, 128, BYTES, true, false>(a, 0, fast, st);
+  } else {
+    launch_tiles<128, 128, BYTES, false, false>(a, 0, fast, st);
+  }
+}
+
+void launch_tile(const ProductArgs& a, const ProductPlan& plan, bool fast, hipStream_t st) {
   if (a.splits == 1) {
-    if (a.c_bf16) launch_tile_kind<2>(a, large, fast, st);
-    else launch_tile_kind<4>(a, large, fast, st);
+    if (a.c_bf16) launch_tile_kind<2>(a, plan, fast, st);
+    else launch_tile_kind<4>(a, plan, fast, st);
     return;
   }
   ProductArgs parts = a;
@@ -617,7 +638,7 @@ void launch_tile(const ProductArgs& a, bool large, bool fast, hipStream_t st) {
   parts.c_vec = 1;
   parts.n = (uint32_t)a.part_stride;  // columns past b's last one: sums of zeros
   parts.accumulate = 0;
-  launch_tile_kind<4>(parts, large, fast, st);
+  launch_tile_kind<4>(parts, plan, fast, st);
   hipLaunchKernelGGL(join_splits_kernel, dim3((uint32_t)std::min<int64_t>(2048, ceil_div(a.m * (a.part_stride / 4), 256))), dim3(256), 0, st, a);
 }
 
@@ -653,7 +674,7 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
     if (l.n * (int64_t)size % 16) a.c_vec = 0;  // whole pieces only
     a.part = static_cast<float*>(l.workspace);
     a.part_stride = part_stride(l.n);
-    launch_tile(a, plan.kind == ProductPlan::kTile256, l.fast, st);
+    launch_tile(a, plan, l.fast, st);
   } else {
     if (l.m <= 16) launch_few_rows<1, kCodes>(a, l.fast, st);
     else launch_few_rows<2, kCodes>(a, l.fast, st);

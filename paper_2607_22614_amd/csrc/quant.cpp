@@ -120,24 +120,33 @@ int check_workspace(const void* p, uint64_t have, uint64_t need, const char* wha
 // tile alone on its CU 0.63 (0.78) and of two of them together 0.96 (1.72); what a tile costs beside its steps 8 and 1.5;
 // a launch 4; joining splits 2.5 and their sums' bytes, written and read, at 6.5 TB/s.
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
-  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
+  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.63 : 0.78, pair128 = fast ? 0.96 : 1.72;
-  ProductPlan best{ProductPlan::kTile256, 1};
+  ProductPlan best{ProductPlan::kTile256, 1, 0};
   double least = HUGE_VAL;
   for (const auto kind : {ProductPlan::kTile256, ProductPlan::kTile128}) {
     const int64_t side = kind == ProductPlan::kTile256 ? 256 : 128;
     const double tiles = (double)ceil_div(m, side) * (double)ceil_div(n, side);
     for (uint32_t splits = 1; splits <= 16 && (splits == 1 || kb >= 2 * (int64_t)splits); ++splits) {
       const double steps = (double)ceil_div(kb, splits), rounds = std::ceil(tiles * splits / kCus);
-      double us = splits == 1 ? 0 : 2.5 + 8.0 * splits * (double)m * (double)part_stride(n) / 6.5e6;
-      if (kind == ProductPlan::kTile256) {
-        us += rounds * (steps * step256 + 8);
-      } else {
-        const double pairs = std::floor(rounds / 2), lone = rounds - 2 * pairs;
-        us += pairs * (steps * pair128 + 1.5) + lone * (steps * step128 + 1.5);
+      const double us = splits == 1 ? 0 : 2.5 + 8.0 * splits * (double)m * (double)part_stride(n) / 6.5e6;
+      auto time128 = [&](double n_rounds) {
+        const double pairs = std::floor(n_rounds / 2), lone = n_rounds - 2 * pairs;
+        return pairs * (steps * pair128 + 1.5) + lone * (steps * step128 + 1.5);
+      };
+      auto consider = [&](double time, uint32_t quartered) {
+        if (us + time < least) least = us + time, best = {kind, splits, quartered};
+      };
+      if (kind == ProductPlan::kTile128) {
+        consider(time128(rounds), 0);
+        continue;
       }
-      if (us < least) least = us, best = {kind, splits};
+      const double round = steps * step256 + 8, rest = tiles - kCus * (rounds - 1);
+      consider(rounds * round, 0);
+      // a last round that few tiles share: these by quarters
+      if (splits == 1 && rounds > 1 && rest < kCus)
+        consider((rounds - 1) * round + 4 + time128(std::ceil(4 * rest / kCus)), (uint32_t)rest);
     }
   }
   return best;

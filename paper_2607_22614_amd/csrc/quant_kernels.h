@@ -52,10 +52,12 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st);
 constexpr uint32_t kFusedRows = 16;
 
 // How a product of 8-bit operands is cut: tiles of one of two sizes, and each tile's blocks over `splits` workgroups
-// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows.
+// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows.  The last `quartered`
+// tiles of 256 x 256 are cut into tiles of 128 x 128 each.
 struct ProductPlan {
   enum Kind { kDirect, kTile128, kTile256 } kind;
   uint32_t splits;
+  uint32_t quartered;
 };
 inline int64_t part_stride(int64_t n) { return ceil_div(n, 4) * 4; }
 

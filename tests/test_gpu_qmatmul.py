@@ -324,3 +324,26 @@ def test_on_another_stream_and_in_a_graph():
             graph.replay()
             torch.cuda.synchronize()
             _close(y, *ref(), k, False)
+
+
+@pytest.mark.parametrize("m,n,k", [(4100, 4360, 5120), (5000, 7000, 3000), (4352, 4104, 4000)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_last_tiles_in_quarters(m, n, k, fast):
+    """Somewhat more large tiles than a round of workgroups takes: the others leave as quarters, some of them outside of c."""
+    dr = _dr()
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    x, w = torch.randn((m, k), generator=gen, device="cuda"), torch.randn((n, k), generator=gen, device="cuda")
+    a, b = dr.QMatrix.empty(m, k, 1), dr.QMatrix.empty(n, k, 128)
+    dr.dr_quantize(x, a), dr.dr_quantize(w, b)
+    av = torch.from_numpy(quant.values(a.data.cpu().numpy(), a.scales.cpu().numpy(), k, 1)).cuda()
+    bv = torch.from_numpy(quant.values(b.data.cpu().numpy(), b.scales.cpu().numpy(), k, 128)).cuda()
+    want, size = av @ bv.t(), av.abs() @ bv.abs().t()
+    tol = ((-(-k // 128) * 128 + 64) * 2.0**-23 + (2.0**-10 if fast else 0)) * size
+    ws = _workspace(dr, m, n, k)
+    for dtype, accumulate in ((torch.bfloat16, False), (torch.float32, False), (torch.float32, True)):
+        say("quarters", m, n, k, fast, dtype, accumulate)
+        buf = torch.full((m + 1, n + 16), 3.0, dtype=dtype, device="cuda")
+        dr.dr_qmatmul(a, b, buf[:m, :n], accumulate=accumulate, fast=fast, workspace=ws)
+        off = (buf[:m, :n].to(torch.float64) - want - (3.0 if accumulate else 0.0)).abs()
+        assert (off <= tol + (want.abs() * 2.0**-8 if dtype == torch.bfloat16 else 2.0**-20)).all()
+        assert (buf[m] == 3.0).all() and (buf[:, n:] == 3.0).all()

@@ -241,13 +241,16 @@ void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
 }
 
 // More columns a workgroup read a fewer times, fewer columns give more workgroups.  One tile of 16 columns up to 4096
-// (256 workgroups), two up to 16384, then four; eight waves share the blocks, four of the widest.  In us for 1 / 2 / 4:
-//   1 row, 4096 x 3584: 5.5 / 7.1 / 10.4     16 rows, 6912 x 5120: 17.0 / 13.0 / 18.3     32 rows, 32064 x 4096: 50 / 37 / 32
-// and with 4 / 8 / 16 waves, 1 row, 4096 x 3584: 6.4 / 5.5 / 5.7; four tiles, 16 rows, 151936 x 896: 29 / 38 / 66.
+// (256 workgroups), two up to 9216, then four; eight waves share the blocks, four of the widest.  In us for 1 / 2 / 4 tiles:
+//   4096 x 3584, 1 row 5.8 / 7.3 / 10.6, 16 rows 8.1 / 9.7 / 12.7     6912 x 5120, 1 row 10.9 / 9.3 / 13.9, 16 rows 17.0 / 12.5 / 16.7
+//   14336 x 4096, 1 row 18.2 / 16.4 / 16.5, 16 rows 25.8 / 20.0 / 17.5     32064 x 4096, 16 rows 48 / 36 / 31
+// and with 4 / 8 / 16 waves, 1 row, 4096 x 3584: 6.6 / 5.8 / 6.1; four tiles with 2 / 4 / 8, 16 rows, 151936 x 896: 33 / 32 / 41.
+//   Bound by how fast the weights come, up to 5.2 TB/s (1 row, 151936 x 896: 26 us), and at 16 rows by x, which every
+// workgroup reads: 6912 x 5120 take 9.3 us for one row.  More blocks in flight per wave (2 to 6) lost 5 to 50 %.
 template <int TT, int X>
 void launch_few_rows(const ProductArgs& a, bool fast, hipStream_t st) {
   if (a.n <= 4096) launch_direct<1, TT, 8, X>(a, fast, st);
-  else if (a.n <= 16384) launch_direct<2, TT, 8, X>(a, fast, st);
+  else if (a.n <= 9216) launch_direct<2, TT, 8, X>(a, fast, st);
   else launch_direct<4, TT, 4, X>(a, fast, st);
 }
 

@@ -5,7 +5,7 @@
 // exact, so the codes depend on nothing but the definition.
 //
 // HBM-bound: 2 or 4 bytes read and 1 byte written per element and orientation.  8192 x 5120 bf16 along the rows take 23 us
-// (5.5 TB/s), 8192 x 4096 both ways 28 (4.8), 8192 x 14336 95 (5.0): a tile's codes leave only after all of it has come.
+// (5.5 TB/s), 8192 x 4096 both ways 25 to 28 (4.8 to 5.4), 8192 x 14336 95 (5.0): a tile's codes leave only after all of it has come.
 #include <hip/hip_runtime.h>
 
 #include "quant_device.h"
@@ -17,12 +17,16 @@ struct QuantizeArgs {
   const void* src;
   int64_t src_stride;
   uint32_t rows, cols, tiles_x;
-  int32_t aligned;  // rows begin at whole 16 bytes
+  int32_t stream;
   QView q, qt;
 };
 
-// Eight columns of ROWS rows; rows past the matrix read its last one.  Rows at whole 16 bytes are streamed past the caches:
-// 8192 x 5120 bf16 in 23 us, 26 otherwise; rows that share their lines with others take 13 instead of 10 that way.
+// Eight columns of ROWS rows; rows past the matrix read its last one.  The sources of large calls are streamed past the
+// caches, where their rows begin at whole 16 bytes (those that share lines with others take 13 instead of 10 us for 3000 x
+// 3001 that way).  Of a call that moves up to kCached bytes in all the source may still lie in the last cache (256 MiB),
+// where the call that wrote it left it: 7168 x 4096 bf16 then take 14 us and streamed 16, from HBM 19 and 17; 8192 x 4096
+// both ways 28 and 25.
+constexpr int64_t kCached = 96ll << 20;
 template <bool BF16, int ROWS>
 __device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, uint32_t col, Raw8<BF16> (&v)[ROWS]) {
   auto each = [&](auto load) {
@@ -30,7 +34,7 @@ __device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, 
     for (int i = 0; i < ROWS; ++i) v[i] = load(a.src, (int64_t)min(row0 + i, a.rows - 1) * a.src_stride, col, a.cols);
   };
   if (a.cols < 8) each(load_short_row8<BF16>);
-  else if (a.aligned) each(load_row8<BF16, true>);
+  else if (a.stream) each(load_row8<BF16, true>);
   else each(load_row8<BF16>);
   const uint32_t s = ahead8(col, a.cols);
   if (__any(s)) {
@@ -223,7 +227,9 @@ hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
   a.cols = l.cols;
   a.q = l.q;
   a.qt = l.qt;
-  a.aligned = reinterpret_cast<uintptr_t>(l.src) % 16 == 0 && l.src_stride % (l.bf16 ? 8 : 4) == 0;
+  const int64_t size = l.bf16 ? 2 : 4;
+  const int64_t moved = (int64_t)l.rows * l.cols * (size + (l.q.data != nullptr) + (l.qt.data != nullptr));
+  a.stream = moved > kCached && reinterpret_cast<uintptr_t>(l.src) % 16 == 0 && l.src_stride * size % 16 == 0;
   const bool square = (l.q.data ? l.q.sh : l.qt.sh) != 0;
   if (!square && !l.qt.data) {
     a.tiles_x = (uint32_t)ceil_div(l.cols, 512);

@@ -120,3 +120,25 @@ def test_empty_matrices_are_left_alone():
         q, qt = dr.QMatrix.empty(rows, cols, 1), dr.QMatrix.empty(cols, rows, 1)
         dr.dr_quantize(torch.empty((rows, cols), device="cuda"), q, qt)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(8197, 5128), (12800, 4104)])
+def test_large_calls(rows, cols, dtype):
+    """Sources that are streamed past the caches: the same codes as of any part of them."""
+    from oracle import quant
+    from paper_2607_22614_amd import dr
+    say("large", rows, cols, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn((rows, cols), generator=gen, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    x[rows - 3, 5] = float("inf")
+    q, qt = dr.QMatrix.empty(rows, cols, 1), dr.QMatrix.empty(cols, rows, 1)
+    dr.dr_quantize(x, q, qt)
+    alone = dr.QMatrix.empty(rows, cols, 1)
+    dr.dr_quantize(x, alone)
+    assert torch.equal(alone.data, q.data) and torch.equal(alone.scales, q.scales)
+    for m, src in ((q, x), (qt, x.t())):
+        for part in (slice(0, 40), slice(m.rows - 40, m.rows)):
+            codes, scales = quant.quantize(src[part].to(torch.float64).cpu().numpy(), 1)
+            assert (m.data[part].cpu().numpy() == codes).all()
+            assert (m.scales[:, part].cpu().numpy() == scales).all()

@@ -266,14 +266,20 @@ __device__ __forceinline__ Buffer buffer_at(const uint8_t* base, uint32_t bytes)
 __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lane_at, uint32_t at, uint8_t* to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)lane_at, (int)at, 0, 0);
 }
+// 4 bytes per lane.
+__device__ __forceinline__ void copy_words_to_lds(Buffer from, uint32_t lane_at, uint32_t at, uint8_t* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 4, (int)lane_at, (int)at, 0, 0);
+}
 
-// Every wave's copies have landed, and all of them see that.  The wait is written out: a barrier alone orders the LDS
-// accesses that the compiler sees, and leaves copies to LDS on their way.
+// Every wave's copies but the LEFT latest ones have landed, and all of them see that; all LDS reads are done.  The wait is
+// written out: a barrier alone orders the LDS accesses that the compiler sees, and leaves copies to LDS on their way.
+template <int LEFT = 0>
 __device__ __forceinline__ void landed_barrier() {
+  static_assert(LEFT < 64, "a 6-bit counter");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), the other counters as they are
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LEFT & 15) | (LEFT >> 4) << 14);  // vmcnt(LEFT), lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  __syncthreads();
 }
 
 // Work item b of a product: a tile (m0, n0) and its blocks [j0, j1), one split's.  Each XCD takes a contiguous eighth
@@ -291,7 +297,7 @@ __device__ __forceinline__ Item item_of(const ProductArgs& p, uint32_t b) {
   const uint32_t at = xcd_tile(b, items_of(p)), part = at & (p.quarters * 3), all = at >> 2 * p.quarters;
   const uint32_t split = all / p.count, t = p.first + all % p.count;
   const uint32_t band = t / (kBand * p.tiles_n), high = min(kBand, p.tiles_m - band * kBand), i = t - band * kBand * p.tiles_n;
-  const uint32_t y = (band * kBand + i % high << p.quarters) + part % 2, x = (i / high << p.quarters) + part / 2;
+  const uint32_t y = ((band * kBand + i % high) << p.quarters) + part % 2, x = (i / high << p.quarters) + part / 2;
   // the same for the whole workgroup, which the compiler does not see behind the divisions
   return Item{same(y * BM), same(x * BN), same(split), same((uint32_t)((uint64_t)p.kb * split / p.splits)),
               same((uint32_t)((uint64_t)p.kb * (split + 1) / p.splits))};
@@ -378,17 +384,22 @@ __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 
 // 2 % 8: the sixteen lanes that read at once, the same piece of sixteen rows, then meet all 64 banks.  The copies run two
 // blocks ahead of the products and through the ends of tiles: while a tile's results leave, the next one's first blocks
 // are on their way.  Every item has two blocks or more, or (ONE) a single one.
+//   S > 2: that many buffers, for workgroups that have a CU to themselves and take one item each.  The copies then run S
+// blocks ahead, and the scale codes come with them, a word (four blocks' codes) per row: loaded to registers they would have
+// to wait for the copies before them.
 //   Long products are bound by power: 8192 x 14336 x 4096 take 385 us (2500 TFLOP/s) with the matrix units busy 64 % of the
 // cycles at a clock of about 1.8 GHz, exact sums 700 to 750 us.  Few rows are bound by how fast b comes: 61 x 151936 x 896
 // 36 us (4.7 TB/s); short K by the start and end of tiles: 768 x 9728 x 896 13 us.
-template <int BM, int BN, int WM, int WN, int BYTES, bool VEC, bool FAST, bool ONE>
+template <int BM, int BN, int WM, int WN, int BYTES, bool VEC, bool FAST, bool ONE, int S>
 __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs p) {
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, kRows = BM + BN, kCopies = kRows / 8 / kWaves;
   static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && kRows % (8 * kWaves) == 0 && BM % (8 * kWaves) == 0, "tile");
-  // two stages, and each wave's part for its results: one array, since between accesses to arrays that it can tell apart
+  // the stages, and each wave's part for its results: one array, since between accesses to arrays that it can tell apart
   // the compiler waits for the copies on their way
-  constexpr int kStage = kRows * 128;
-  __shared__ __align__(16) uint8_t lds[2 * kStage + kWaves * TN * 2048];
+  constexpr bool DEEP = S > 2;
+  constexpr int kStage = kRows * (DEEP ? 132 : 128), kCodes = kRows * 128, kPerStep = kCopies + 1;  // (DEEP) copies of a step
+  static_assert(!DEEP || (kRows == 64 * kWaves && BM % 64 == 0 && !ONE), "a wave copies the codes of 64 rows of one side");
+  __shared__ __align__(16) uint8_t lds[S * kStage + kWaves * TN * 2048];
   const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t wm = wave % WM * (TM * 32), wn = wave / WM * (TN * 32);
@@ -424,6 +435,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     copy_to_lds(i * kWaves * 8 < BM ? buffer_at(source.a, source.abytes) : buffer_at(source.b, source.bbytes), from[i], source.block * 128,
                 to + (i * kWaves + wave) * 1024);
   };
+  const bool a_codes = wave * 64 < BM;
+  const uint32_t code_at = 4 * (a_codes ? (wave * 64 + lane) >> p.a.sh : (wave * 64 + lane - BM) >> p.b.sh);
+  auto stage_codes = [&](uint8_t* to) {
+    if (a_codes) copy_words_to_lds(ascales, code_at, source.acodes + source.block / 4 * p.a.srows * 4, to + kCodes + wave * 256);
+    else copy_words_to_lds(bscales, code_at, source.bcodes + source.block / 4 * p.b.srows * 4, to + kCodes + wave * 256);
+  };
   // to the next block, or the first one of the upcoming item
   auto advance = [&] {
     const bool same = ++source.block < source.end;
@@ -447,6 +464,17 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     for (int t = 0; t < TM; ++t) s.a[t] = __builtin_amdgcn_raw_buffer_load_b8(ascales, (int)acode[t], (int)aat, 0);
 #pragma unroll
     for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)bcode[t], (int)bat, 0);
+    return s;
+  };
+
+  // (DEEP) of the block staged at `from_lds`
+  auto read_scales = [&](const uint8_t* from_lds, uint32_t block) {
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(from_lds + kCodes);
+    Scales s;
+#pragma unroll
+    for (int t = 0; t < TM; ++t) s.a[t] = (int)(words[wm + t * 32 + r] >> block % 4 * 8 & 255);
+#pragma unroll
+    for (int t = 0; t < TN; ++t) s.b[t] = (int)(words[BM + wn + t * 32 + r] >> block % 4 * 8 & 255);
     return s;
   };
 
@@ -495,23 +523,27 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   Codes first;
   Scales now, next;
   uint32_t in = 0;
-  auto step = [&] {
-    uint8_t *cur = lds + in * kStage, *other = lds + (in ^ 1) * kStage;
+  auto step = [&](uint32_t following) {  // the block after this one
+    const uint32_t in_next = in + 1 == S ? 0 : in + 1;
+    uint8_t *cur = lds + in * kStage, *other = lds + in_next * kStage;
     Codes second;
     multiply(first, now, [&](int i) {
 #pragma unroll
       for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) second.piece[k] = read_piece(cur, 1, k);
     });
-    landed_barrier();
+    landed_barrier<DEEP ? (S - 2) * kPerStep : 0>();
     __builtin_amdgcn_sched_barrier(0);
-    // used from here on only: copied any earlier, they would be waited for there, and all copies with them
+    if constexpr (!DEEP) {
+      // used from here on only: copied any earlier, they would be waited for there, and all copies with them
 #pragma unroll
-    for (int t = 0; t < TM; ++t) asm volatile("" : "+v"(next.a[t]));
+      for (int t = 0; t < TM; ++t) asm volatile("" : "+v"(next.a[t]));
 #pragma unroll
-    for (int t = 0; t < TN; ++t) asm volatile("" : "+v"(next.b[t]));
-    const Scales landed = next;
+      for (int t = 0; t < TN; ++t) asm volatile("" : "+v"(next.b[t]));
+    }
+    const Scales landed = DEEP ? read_scales(other, following) : next;
     advance();
-    next = load_scales();
+    if constexpr (DEEP) stage_codes(cur);
+    else next = load_scales();
     multiply(second, now, [&](int i) {
 #pragma unroll
       for (int k = i * kPieces / kTiles; k < (i + 1) * kPieces / kTiles; ++k) first.piece[k] = read_piece(other, 0, k);
@@ -519,12 +551,25 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
       for (int k = i * kCopies / kTiles; k < (i + 1) * kCopies / kTiles; ++k) stage(cur, k);
     });
     now = landed;
-    in ^= 1;
+    in = in_next;
   };
 
+  // behind the last item: nothing of its rows is there, and copies of them take no memory access
+  auto no_more = [&] { upcoming.abytes = upcoming.bbytes = 0; };
   Item t = item_of<BM, BN>(p, blockIdx.x);
   source = upcoming = source_of(t);
-  if constexpr (!ONE) {
+  if constexpr (DEEP) {
+    no_more();
+#pragma unroll
+    for (int b = 0; b < S; ++b) {
+      if (b) advance();
+      stage_codes(lds + b * kStage);
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) stage(lds + b * kStage, i);
+    }
+    landed_barrier<(S - 1) * kPerStep>();
+    now = read_scales(lds, t.j0);
+  } else if constexpr (!ONE) {
     now = load_scales();
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) stage(lds, i);
@@ -533,6 +578,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) stage(lds + kStage, i);
     landed_barrier();
+  }
+  if constexpr (!ONE) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) first.piece[i] = read_piece(lds, 0, i);
   }
@@ -542,9 +589,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
 #pragma unroll
       for (int y = 0; y < TM; ++y) acc[x][y] = f32x16{};
     const Item done = t;
-    // behind the last item its own blocks are copied once more
-    if (b + gridDim.x < items) t = item_of<BM, BN>(p, b + gridDim.x);
+    const bool more = b + gridDim.x < items;
+    if (more) t = item_of<BM, BN>(p, b + gridDim.x);
     upcoming = source_of(t);
+    if (!more) no_more();
     if constexpr (ONE) {
       __syncthreads();  // every wave has read the block before
       now = load_scales();
@@ -560,7 +608,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
       source = upcoming;
     } else {
       uint32_t j = done.j0;
-      do step();
+      do step(j + 1);
       while (++j < done.j1);
     }
     // the results are read by instructions written out (bf16_pair_here), whose distance from the matrix instructions that
@@ -573,7 +621,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     asm volatile("" : "+v"(me));
     ProductArgs out = p;
     out.c = static_cast<uint8_t*>(p.c) + done.split * p.split_bytes;
-    store_turned<TM, TN, BYTES, VEC>(out, acc, lds + 2 * kStage + wave * TN * 2048, done.m0 + wm, done.n0 + wn, me);
+    store_turned<TM, TN, BYTES, VEC>(out, acc, lds + S * kStage + wave * TN * 2048, done.m0 + wm, done.n0 + wn, me);
   }
   landed_barrier();  // no copy is on its way any more when the LDS goes to another workgroup
 }
@@ -591,13 +639,25 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs p) {
   }
 }
 
+// Workgroups with a CU to themselves stage four blocks, in the LDS of the second one that is not there: fast sums of 512 x
+// 6912 x 5120 in 24 us instead of 35, 100 x 32064 x 4096 37 (46), 2048 x 2000 x 2000 14 (17).  Exact sums are not faster (512 x
+// 896 x 4864 20.6 and 19.9), nor are items of two or three blocks (200 x 688 x 256 5.7 and 5.4).
+constexpr uint32_t kCus = 256;
+constexpr int kDeep = 4;
 template <int BM, int BN, int BYTES, bool VEC, bool ONE>
 void launch_items(const ProductArgs& a, bool fast, hipStream_t st) {
-  // as many workgroups as the LDS of 256 CUs holds; a multiple of the XCDs keeps a workgroup's items on its XCD
-  constexpr uint32_t kResident = 256 * (160 / ((BM + BN) / 4 + BN / 8));
-  const dim3 grid(std::min(a.count * a.splits << 2 * a.quarters, kResident)), block(256);
-  if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, true, ONE>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, false, ONE>), grid, block, 0, st, a);
+  // as many workgroups as the LDS of all CUs holds; a multiple of the XCDs keeps a workgroup's items on its XCD
+  constexpr uint32_t kResident = kCus * (160 / ((BM + BN) / 4 + BN / 8));
+  const uint32_t items = a.count * a.splits << 2 * a.quarters;
+  const dim3 grid(std::min(items, kResident)), block(256);
+  if constexpr (BM + BN == 256 && !ONE) {
+    if (fast && items <= kCus && a.kb >= kDeep * a.splits) {
+      hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, true, false, kDeep>), grid, block, 0, st, a);
+      return;
+    }
+  }
+  if (fast) hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, true, ONE, 2>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((product_tile_kernel<BM, BN, 2, 2, BYTES, VEC, false, ONE, 2>), grid, block, 0, st, a);
 }
 
 // All tiles but the last `quartered` ones of 256 x 256, and these as tiles of 128 x 128 in a second launch, two to a CU:

@@ -117,9 +117,10 @@ int check_workspace(const void* p, uint64_t have, uint64_t need, const char* wha
 }  // namespace
 
 // Times of a workgroup in us, measured on random codes: a step of a 256 x 256 tile 1.34 (exact sums 2.7), of one 128 x 128
-// tile alone on its CU 0.63 (0.78) and of two of them together 0.96 (1.72); what a tile costs beside its steps 8, 3 and, of
-// two together, 4; a second launch 6; joining splits 4 and their sums' bytes, written and read, at 6.5 TB/s.  Over 74 shapes from
-// 48 x 9728 x 896 to 3000 x 14336 x 4096 the choice takes at most 13 % more than the best of eight.
+// tile alone on its CU 0.63 (0.78; 0.5 with four blocks staged) and of two of them together 0.96 (1.72); what a tile costs
+// beside its steps 8, 3 and, of two together, 4; a second launch 6; joining splits 4 and their sums' bytes, written and
+// read, at 6.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice takes at most 14 % more than the
+// best of eight.
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
   if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
   constexpr double kCus = 256;
@@ -134,7 +135,8 @@ ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
       const double us = splits == 1 ? 0 : 4 + 8.0 * splits * (double)m * (double)part_stride(n) / 6.5e6;
       auto time128 = [&](double n_rounds) {
         const double pairs = std::floor(n_rounds / 2), lone = n_rounds - 2 * pairs;
-        return pairs * (steps * pair128 + 4) + lone * (steps * step128 + 3);
+        const double step = fast && n_rounds == 1 && steps >= 4 ? 0.5 : step128;
+        return pairs * (steps * pair128 + 4) + lone * (steps * step + 3);
       };
       auto consider = [&](double time, uint32_t quartered) {
         if (us + time < least) least = us + time, best = {kind, splits, quartered};

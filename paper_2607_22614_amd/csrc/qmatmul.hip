@@ -130,7 +130,7 @@ __device__ __forceinline__ i32x8 quantize_block(const Elements<X>& e, int& code)
   return w;
 }
 
-// Few rows: a tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
+// Few rows, or few results: a tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
 // instructions; the KS waves of the workgroup take the 128-column blocks in turn, each with its next block in flight while
 // it multiplies one, and join their sums in LDS, in the order of the waves.  X: a's codes, or rows of x to quantize.
 template <int FT, int TT, int KS, int X, bool FAST>
@@ -249,9 +249,10 @@ void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
 // workgroup reads: 6912 x 5120 take 9.3 us for one row.  More blocks in flight per wave (2 to 6) lost 5 to 50 %.
 template <int TT, int X>
 void launch_few_rows(const ProductArgs& a, bool fast, hipStream_t st) {
-  if (a.n <= 4096) launch_direct<1, TT, 8, X>(a, fast, st);
-  else if (a.n <= 9216) launch_direct<2, TT, 8, X>(a, fast, st);
-  else launch_direct<4, TT, 4, X>(a, fast, st);
+  const uint32_t columns16 = direct_columns16(a.n);
+  if (columns16 == 1) launch_direct<1, TT, direct_waves(1), X>(a, fast, st);
+  else if (columns16 == 2) launch_direct<2, TT, direct_waves(2), X>(a, fast, st);
+  else launch_direct<4, TT, direct_waves(4), X>(a, fast, st);
 }
 
 // ------------------------------------------------------------------ large products
@@ -743,8 +744,12 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
     a.part_stride = part_stride(l.n);
     launch_tile(a, plan, l.fast, st);
   } else {
-    if (l.m <= 16) launch_few_rows<1, kCodes>(a, l.fast, st);
-    else launch_few_rows<2, kCodes>(a, l.fast, st);
+    switch (plan.rows16) {
+      case 1: launch_few_rows<1, kCodes>(a, l.fast, st); break;
+      case 2: launch_few_rows<2, kCodes>(a, l.fast, st); break;
+      case 3: launch_few_rows<3, kCodes>(a, l.fast, st); break;
+      default: launch_few_rows<4, kCodes>(a, l.fast, st);
+    }
   }
   return hipGetLastError();
 }

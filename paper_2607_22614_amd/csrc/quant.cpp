@@ -116,17 +116,27 @@ int check_workspace(const void* p, uint64_t have, uint64_t need, const char* wha
 
 }  // namespace
 
-// Times of a workgroup in us, measured on random codes: a step of a 256 x 256 tile 1.34 (exact sums 2.7), of one 128 x 128
-// tile alone on its CU 0.63 (0.78; 0.5 with four blocks staged) and of two of them together 0.96 (1.72); what a tile costs
-// beside its steps 8, 3 and, of two together, 4; a second launch 6; joining splits 4 and their sums' bytes, written and
-// read, at 6.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice takes at most 14 % more than the
-// best of eight.
+// Times in us, measured on random codes.  A step of a 256 x 256 tile takes 1.34 (exact sums 2.7), of one 128 x 128 tile
+// alone on its CU 0.63 (0.78; 0.5 with four blocks staged) and of two of them together 0.96 (1.72); what a tile costs beside
+// its steps is 8, 3 and, of two together, 4; a second launch 6; joining splits 4 and their sums' bytes, written and read, at
+// 6.5 TB/s.  A round of 256 workgroups of the kernel for few rows takes direct_step (by columns and by rows per workgroup)
+// for each 128-column block of a wave, beside direct_start and 0.5 for each further round, and no less than the weights at
+// 4.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice among tiles takes at most 14 % more than
+// the best of eight; with the kernel for few rows 64 x 2000 x 2000 6.6 instead of 11.0, 200 x 688 x 256 3.6 (5.4).
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
-  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0};  // 48 rows, 6912 x 5120: 18-20 us, by tiles of 128 19
+  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0, m <= 16 ? 1u : 2u};
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.63 : 0.78, pair128 = fast ? 0.96 : 1.72;
-  ProductPlan best{ProductPlan::kTile256, 1, 0};
+  ProductPlan best{ProductPlan::kTile256, 1, 0, 2};
   double least = HUGE_VAL;
+  constexpr double direct_step[3][3] = {{1.45, 1.72, 2.45}, {1.88, 2.3, 2.9}, {1.35, 1.75, 2.1}}, direct_start[3] = {1.8, 3, 3};
+  const uint32_t columns16 = direct_columns16(n), waves = direct_waves(columns16), wide = columns16 / 2;
+  const double blocks = kb < waves ? (double)kb / waves : (double)ceil_div(kb, waves);
+  for (uint32_t rows16 = 2; rows16 <= 4; ++rows16) {
+    const double rounds = std::ceil((double)ceil_div(n, 16 * columns16) * (double)ceil_div(m, 16 * rows16) / kCus);
+    const double us = std::max(direct_start[wide] + rounds * blocks * direct_step[wide][rows16 - 2] + 0.5 * (rounds - 1), 2 + 128.0 * (double)kb * (double)n / 4.5e6);
+    if (us < least) least = us, best = {ProductPlan::kDirect, 1, 0, rows16};
+  }
   for (const auto kind : {ProductPlan::kTile256, ProductPlan::kTile128}) {
     const int64_t side = kind == ProductPlan::kTile256 ? 256 : 128;
     const double tiles = (double)ceil_div(m, side) * (double)ceil_div(n, side);
@@ -139,7 +149,7 @@ ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
         return pairs * (steps * pair128 + 4) + lone * (steps * step + 3);
       };
       auto consider = [&](double time, uint32_t quartered) {
-        if (us + time < least) least = us + time, best = {kind, splits, quartered};
+        if (us + time < least) least = us + time, best = {kind, splits, quartered, 2};
       };
       if (kind == ProductPlan::kTile128) {
         consider(time128(rounds), 0);

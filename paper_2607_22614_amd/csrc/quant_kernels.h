@@ -52,13 +52,18 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st);
 constexpr uint32_t kFusedRows = 16;
 
 // How a product of 8-bit operands is cut: tiles of one of two sizes, and each tile's blocks over `splits` workgroups
-// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows.  The last `quartered`
-// tiles of 256 x 256 are cut into tiles of 128 x 128 each.
+// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows, `rows16` times 16 of them
+// per workgroup.  The last `quartered` tiles of 256 x 256 are cut into tiles of 128 x 128 each.
 struct ProductPlan {
   enum Kind { kDirect, kTile128, kTile256 } kind;
   uint32_t splits;
   uint32_t quartered;
+  uint32_t rows16;  // of kDirect: 1 to 4
 };
+// Tiles of 16 columns per workgroup of the kernel for few rows, and its waves, by the columns of c.
+inline uint32_t direct_columns16(int64_t n) { return n <= 4096 ? 1 : n <= 9216 ? 2 : 4; }
+constexpr uint32_t direct_waves(uint32_t columns16) { return columns16 == 4 ? 4 : 8; }
+
 inline int64_t part_stride(int64_t n) { return ceil_div(n, 4) * 4; }
 
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast);

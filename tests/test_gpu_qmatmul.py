@@ -347,3 +347,68 @@ def test_last_tiles_in_quarters(m, n, k, fast):
         off = (buf[:m, :n].to(torch.float64) - want - (3.0 if accumulate else 0.0)).abs()
         assert (off <= tol + (want.abs() * 2.0**-8 if dtype == torch.bfloat16 else 2.0**-20)).all()
         assert (buf[m] == 3.0).all() and (buf[:, n:] == 3.0).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(509, 2008, 1990), (509, 2003, 512), (1200, 2000, 2000), (130, 6903, 5100), (517, 905, 4900), (260, 2600, 640), (2000, 1999, 385)])
+@pytest.mark.parametrize("blocks", [(1, 128), (1, 1), (128, 128)])
+def test_workgroups_with_a_cu_to_themselves(m, n, k, blocks):
+    """Up to 256 tiles, whole or split along K, of four blocks and more: at the edges of c, with every kind of scales."""
+    dr = _dr()
+    a, av = _matrix(dr, m, k, blocks[0], m + k, spread=5, extra=16)
+    b, bv = _matrix(dr, n, k, blocks[1], n + k + 1, spread=5, extra=48)
+    av, bv = torch.from_numpy(av).cuda(), torch.from_numpy(bv).cuda()
+    want, size = av @ bv.t(), av.abs() @ bv.abs().t()
+    ws = _workspace(dr, m, n, k)
+    for fast in (True, False):
+        tol = ((-(-k // 128) * 128 + 64) * 2.0**-23 + (2.0**-10 if fast else 0)) * size
+        for dtype, accumulate in ((torch.bfloat16, False), (torch.float32, False), (torch.float32, True)):
+            say("alone on a CU", m, n, k, blocks, fast, dtype, accumulate)
+            buf = torch.full((m + 1, n), 3.0, dtype=dtype, device="cuda")
+            dr.dr_qmatmul(a, b, buf[:m], accumulate=accumulate, fast=fast, workspace=ws)
+            off = (buf[:m].to(torch.float64) - want - (3.0 if accumulate else 0.0)).abs()
+            assert (off <= tol + (want.abs() * 2.0**-8 if dtype == torch.bfloat16 else 2.0**-20)).all()
+            assert (buf[m] == 3.0).all()
+
+
+@pytest.mark.parametrize("m,n", [(700, 2000), (700, 2001), (4100, 4360)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_extreme_scales_and_nan_in_tiles(m, n, fast):
+    dr = _dr()
+    say("extreme scales in tiles", m, n, fast)
+    k = 640
+    a, b = dr.QMatrix.empty(m, k, 1), dr.QMatrix.empty(n, k, 1)
+    a.data.fill_(0x38), b.data.fill_(0x38)  # 1.0
+    ws = _workspace(dr, m, n, k)
+    out = torch.empty((m, n), device="cuda")
+    for ea, eb, want in ((0, 254, 640.0), (127, 127, 640.0), (0, 127, 640 * 2.0**-127), (247, 7, 640.0), (254, 254, float("inf"))):
+        a.scales.fill_(ea), b.scales.fill_(eb)
+        dr.dr_qmatmul(a, b, out, fast=fast, workspace=ws)
+        assert (out == want).all(), (ea, eb, out.flatten()[0].item())
+    a.scales.fill_(127), b.scales.fill_(127)
+    a.data[m - 1, 300] = 0x7F
+    b.data[n - 1, 5] = 0xFF
+    dr.dr_qmatmul(a, b, out, fast=fast, workspace=ws)
+    nan = torch.isnan(out)
+    assert nan[m - 1].all() and nan[:, n - 1].all() and int(nan.sum()) == m + n - 1
+
+
+@pytest.mark.parametrize("m", [33, 47, 63, 64, 130])
+@pytest.mark.parametrize("n,k", [(1000, 130), (4097, 264), (9217, 900), (200, 3000)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_small_products(m, n, k, fast):
+    """Two, three and four times 16 rows a workgroup."""
+    dr = _dr()
+    a, av = _matrix(dr, m, k, 1, m + k, spread=5)
+    b, bv = _matrix(dr, n, k, 128, n + k + 1, spread=5)
+    want, size = quant.product(av, bv)
+    ws = _workspace(dr, m, n, k)
+    for dtype in (torch.float32, torch.bfloat16):
+        say("small", m, n, k, fast, dtype)
+        out = torch.full((m + 1, n), 7.0, dtype=dtype, device="cuda")
+        dr.dr_qmatmul(a, b, out[:m], fast=fast, workspace=ws)
+        torch.cuda.synchronize()
+        if fast:  # 2^-10 of each group's largest product, at most of the sum of magnitudes
+            _close(out[:m], want, size * (1 + 2.0**-10 / ((-(-k // 128) * 128 + 64) * 2.0**-23)), k, dtype == torch.bfloat16)
+        else:
+            _close(out[:m], want, size, k, dtype == torch.bfloat16)
+        assert (out[m] == 7.0).all()

@@ -170,24 +170,18 @@ __device__ __forceinline__ u32x2 row_codes(const Raw8<BF16>& v, uint32_t code) {
   return u32x2{to_e4m3_f32(a[0], a[1], a[2], a[3], s), to_e4m3_f32(b[0], b[1], b[2], b[3], s)};
 }
 
-// Codes of column j of 8 rows.
+// Codes of column j of 4 rows.
 template <bool BF16>
-__device__ __forceinline__ u32x2 column_codes(const Raw8<BF16> (&v)[8], int j, uint32_t code) {
+__device__ __forceinline__ uint32_t column_codes(const Raw8<BF16> (&v)[4], int j, uint32_t code) {
   const float s = scale_operand(code);
-  u32x2 r;
+  if (BF16) {
+    uint32_t pair[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (BF16) {
-      uint32_t pair[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)  // (lower, upper) halves of two rows side by side
-        pair[i] = __builtin_amdgcn_perm(v[4 * h + 2 * i + 1].w[0][j / 2], v[4 * h + 2 * i].w[0][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-      r[h] = to_e4m3_bf16(pair[0], pair[1], s);
-    } else {
-      r[h] = to_e4m3_f32(bits_of<BF16>(v[4 * h], j), bits_of<BF16>(v[4 * h + 1], j), bits_of<BF16>(v[4 * h + 2], j), bits_of<BF16>(v[4 * h + 3], j), s);
-    }
+    for (int i = 0; i < 2; ++i)  // (lower, upper) halves of two rows side by side
+      pair[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[0][j / 2], v[2 * i].w[0][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+    return to_e4m3_bf16(pair[0], pair[1], s);
   }
-  return r;
+  return to_e4m3_f32(bits_of<BF16>(v[0], j), bits_of<BF16>(v[1], j), bits_of<BF16>(v[2], j), bits_of<BF16>(v[3], j), s);
 }
 
 // fp32 -> bf16, ties to even (the hardware convert).

@@ -82,39 +82,41 @@ __device__ __forceinline__ void put_code(const QView& q, uint32_t i, uint32_t j,
     for (uint32_t k = (j & 3) + 1; k < 4; ++k) p[k] = 127;
 }
 
-// A tile of 128 x 128 per workgroup, each lane 8 columns of 8 rows, kept in registers.  ROWS writes the codes
-// along the rows, COLS the transpose: its codes are packed 8 rows to a word, turned in LDS (one 128-byte row per
-// column, 8-byte pieces spread by an exclusive or so that a wave's stores meet no bank twice), and leave as whole
-// 128-byte rows.  SQUARE: one scale for the tile, else one per row (DPP) and one per column (over the four rows of
-// lanes, then over the waves in LDS).
+// A tile of 128 x 128 per workgroup, each lane 8 columns of 4 rows, kept in registers (of 8 rows by half the lanes: 200 x 256
+// bf16 both ways 5.0 us instead of 4.5, 2000 x 4096 fp32 14.1 and 13.4).  ROWS writes the codes along the rows, COLS the
+// transpose: its codes are packed 4 rows to a word, turned in LDS (one 128-byte row per column, its words spread by an
+// exclusive or over the banks), and leave as whole 128-byte rows.  SQUARE: one scale for the tile, else one per row (DPP) and
+// one per column (over the four rows of lanes, then over the waves in LDS).
 //   Tiles go in bands of four down, and 32 of them to an XCD at a time: runs of 512 to 1024 bytes of q's and qt's rows then
 // leave one L2 (8192 x 4096 fp32 both ways 43 us, in the order of the rows 45; 3000 x 3001 bf16 10.8 and 11.6).
 constexpr uint32_t kBandT = 4, kTurn = 32;
+constexpr int kTileThreads = 512;
 template <bool BF16, bool SQUARE, bool ROWS, bool COLS>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
-  __shared__ uint32_t cmax[4][128];
+__global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantizeArgs a) {
+  constexpr int R = 128 / (kTileThreads / 16), kWaves = kTileThreads / 64;
+  __shared__ uint32_t cmax[kWaves][128];
   __shared__ __align__(16) uint8_t turned[COLS ? 128 * 128 : 16];
   const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;
   const uint32_t t = xcd_group<kTurn>(blockIdx.x, gridDim.x), tiles_y = gridDim.x / a.tiles_x, band = t / (kBandT * a.tiles_x);
   const uint32_t high = min(kBandT, tiles_y - band * kBandT), i_band = t - band * kBandT * a.tiles_x;
   const uint32_t rt = band * kBandT + i_band % high, ct = i_band / high;
-  const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * 8;
-  Raw8<BF16> v[8];
+  const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * R;
+  Raw8<BF16> v[R];
   load_rows(a, row0, col, v);
-  if (row0 + 8 > a.rows) {
+  if (row0 + R > a.rows) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < R; ++i)
       if (row0 + i >= a.rows) v[i] = Raw8<BF16>{};
   }
   // the lane's largest magnitude of each row; finite ones only if any is not
-  uint32_t rmax[8], top = 0;
+  uint32_t rmax[R], top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, rmax[i] = row_max(v[i], false));
+  for (int i = 0; i < R; ++i) top = max(top, rmax[i] = row_max(v[i], false));
   const bool odd = __any(top >= kInfBits);
   if (odd) {
     top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, rmax[i] = row_max(v[i], true));
+    for (int i = 0; i < R; ++i) top = max(top, rmax[i] = row_max(v[i], true));
   }
 
   uint32_t square_code = 0;
@@ -122,7 +124,10 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
     const uint32_t m = max_rows(max16(top));
     if ((tid & 63) == 0) cmax[0][wave] = m;
     __syncthreads();
-    square_code = scale_code(max(max(cmax[0][0], cmax[0][1]), max(cmax[0][2], cmax[0][3])));
+    uint32_t most = cmax[0][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) most = max(most, cmax[0][w]);
+    square_code = scale_code(most);
     if (tid == 0) {
       if (ROWS) put_code(a.q, rt, ct, square_code);
       if (COLS) put_code(a.qt, ct, rt, square_code);
@@ -132,13 +137,13 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
   if (ROWS) {
     uint32_t mine = 0;  // of row row0 + tx
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < R; ++i) {
       const uint32_t code = SQUARE ? square_code : scale_code(max16(rmax[i]));
       mine = tx == (uint32_t)i ? code : mine;
       if (row0 + i < a.rows)
         *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = row_codes(v[i], code);
     }
-    if (!SQUARE && tx < 8 && row0 + tx < a.rows) put_code(a.q, row0 + tx, ct, mine);
+    if (!SQUARE && tx < R && row0 + tx < a.rows) put_code(a.q, row0 + tx, ct, mine);
   }
 
   if (COLS) {
@@ -152,7 +157,7 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
 #pragma unroll
         for (int w = 0; w < (BF16 ? 4 : 8); ++w)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) most[w] = larger<BF16>(most[w], magnitude<BF16>(v[i].w[BF16 ? 0 : w / 4][w % 4], finite));
+          for (int i = 0; i < R; ++i) most[w] = larger<BF16>(most[w], magnitude<BF16>(v[i].w[BF16 ? 0 : w / 4][w % 4], finite));
       };
       if (odd) column_max(true);
       else column_max(false);
@@ -174,21 +179,23 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint32_t c = tx * 8 + j;
-        code[j] = scale_code(max(max(cmax[0][c], cmax[1][c]), max(cmax[2][c], cmax[3][c])));
+        uint32_t m = cmax[0][c];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = max(m, cmax[w][c]);
+        code[j] = scale_code(m);
         mine = ty == (uint32_t)j ? code[j] : mine;
       }
       if (ty < 8 && col + ty < a.cols) put_code(a.qt, col + ty, rt, mine);
     }
+    // word ty of a column lies at ty ^ 4 (tx % 8), which keeps its 16-byte pieces together
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<u32x2*>(turned + (tx * 8 + j) * 128 + ((ty ^ tx) * 8)) = column_codes(v, j, code[j]);
+      *reinterpret_cast<uint32_t*>(turned + (tx * 8 + j) * 128 + (ty ^ (tx % 8 * 4)) * 4) = column_codes<BF16>(v, j, code[j]);
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const uint32_t c = r * 32 + tid / 8, piece = tid % 8, x = c / 8;
-      // pieces 2p and 2p+1 lie at (2p)^x and (2p+1)^x: side by side, in turned order where x is odd
-      u32x4 w = *reinterpret_cast<const u32x4*>(turned + c * 128 + ((2 * piece) ^ (x & ~1u)) * 8);
-      if (x & 1) w = u32x4{w[2], w[3], w[0], w[1]};
+    for (int r = 0; r < 128 * 8 / kTileThreads; ++r) {
+      const uint32_t c = r * (kTileThreads / 8) + tid / 8, piece = tid % 8;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(turned + c * 128 + (piece ^ (c / 8 % 8)) * 16);
       if (ct * 128 + c < a.cols)
         *reinterpret_cast<u32x4*>(a.qt.data + (int64_t)(ct * 128 + c) * a.qt.stride + rt * 128 + piece * 16) = w;
     }
@@ -207,7 +214,7 @@ void launch_rows(const QuantizeArgs& a, hipStream_t st) {
 
 template <bool BF16, bool SQUARE>
 void launch_tiles(const QuantizeArgs& a, dim3 grid, hipStream_t st) {
-  const dim3 block(256);
+  const dim3 block(kTileThreads);
   if (a.q.data && a.qt.data) {
     hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, true>), grid, block, 0, st, a);
   } else if (a.qt.data) {

@@ -590,7 +590,8 @@ enum {
  * instructions drop what lies below 2^-13 of the largest product's power of two:
  * at most 2^-10 of sum |a||b|, and 1.5e-5 of the result's norm for normally
  * distributed values, a hundredth of what rounding to bf16 costs.  Without
- * it, or where it brings nothing (few rows), sums lose no more than fp32 does.
+ * it, and where it brings nothing (up to 32 rows of a, and other products
+ * small enough to be computed the same way), sums lose no more than fp32 does.
  * The three products of a linear layer y = x w^T: y = (x, w); dx = dy w = (dy,
  * transpose of w); dw = dy^T x = (transpose of dy, transpose of x).
  *   c: device pointer, aligned to its type.

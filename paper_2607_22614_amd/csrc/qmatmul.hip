@@ -132,8 +132,10 @@ __device__ __forceinline__ i32x8 quantize_block(const Elements<X>& e, int& code)
 
 // Few rows, or few results: a tile of FT * 16 columns by TT * 16 rows of c per workgroup, operands straight from memory to the matrix
 // instructions; the KS waves of the workgroup take the 128-column blocks in turn, each with its next block in flight while
-// it multiplies one, and join their sums in LDS, in the order of the waves.  X: a's codes, or rows of x to quantize.
-template <int FT, int TT, int KS, int X, bool FAST>
+// it multiplies one, and join their sums in LDS, in the order of the waves.  X: a's codes, or rows of x to quantize.  The sums
+// are the exact ones: the 8-bit instructions' would save 6 % at most here (us, theirs / these: 1 x 4096 x 3584 5.9 / 6.1,
+// 16 x 6912 x 5120 13.5 / 13.6, 32 x 6912 x 5120 14.2 / 14.7, 16 x 151936 x 896 33.8 / 34.1, 64 x 2000 x 2000 6.2 / 6.3).
+template <int FT, int TT, int KS, int X>
 __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) {
   __shared__ f32x4 part[KS][FT * TT][64];
   const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -191,24 +193,16 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
         aw[t] = k.a[t];
       }
     }
-    if constexpr (FAST) {
+    Bf16Codes ca[TT];
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
+    for (int t = 0; t < TT; ++t) ca[t] = to_bf16(aw[t], k.ea[t]);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          acc[f][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.b[f], aw[t], acc[f][t], 0, 0, 0, k.eb[f], 0, k.ea[t]);
-    } else {
-      Bf16Codes ca[TT];
+    for (int f = 0; f < FT; ++f) {
+      const Bf16Codes cb = to_bf16(k.b[f], k.eb[f]);
 #pragma unroll
-      for (int t = 0; t < TT; ++t) ca[t] = to_bf16(aw[t], k.ea[t]);
+      for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int f = 0; f < FT; ++f) {
-        const Bf16Codes cb = to_bf16(k.b[f], k.eb[f]);
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.v[i], ca[t].v[i], acc[f][t], 0, 0, 0);
-      }
+        for (int i = 0; i < 4; ++i) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.v[i], ca[t].v[i], acc[f][t], 0, 0, 0);
     }
   };
   if (wave < p.kb) {
@@ -233,11 +227,10 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
 }
 
 template <int FT, int TT, int KS, int X>
-void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
+void launch_direct(ProductArgs a, hipStream_t st) {
   a.tiles_n = (uint32_t)ceil_div(a.n, FT * 16);
   const dim3 grid(a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16)), block(64 * KS);
-  if (fast) hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X, false>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), grid, block, 0, st, a);
 }
 
 // More columns a workgroup read a fewer times, fewer columns give more workgroups.  One tile of 16 columns up to 4096
@@ -248,11 +241,11 @@ void launch_direct(ProductArgs a, bool fast, hipStream_t st) {
 //   Bound by how fast the weights come, up to 5.2 TB/s (1 row, 151936 x 896: 26 us), and at 16 rows by x, which every
 // workgroup reads: 6912 x 5120 take 9.3 us for one row.  More blocks in flight per wave (2 to 6) lost 5 to 50 %.
 template <int TT, int X>
-void launch_few_rows(const ProductArgs& a, bool fast, hipStream_t st) {
+void launch_few_rows(const ProductArgs& a, hipStream_t st) {
   const uint32_t columns16 = direct_columns16(a.n);
-  if (columns16 == 1) launch_direct<1, TT, direct_waves(1), X>(a, fast, st);
-  else if (columns16 == 2) launch_direct<2, TT, direct_waves(2), X>(a, fast, st);
-  else launch_direct<4, TT, direct_waves(4), X>(a, fast, st);
+  if (columns16 == 1) launch_direct<1, TT, direct_waves(1), X>(a, st);
+  else if (columns16 == 2) launch_direct<2, TT, direct_waves(2), X>(a, st);
+  else launch_direct<4, TT, direct_waves(4), X>(a, st);
 }
 
 // ------------------------------------------------------------------ large products
@@ -730,11 +723,11 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   if (l.x) {
     const bool shorter = l.a.cols < 8;
     if (l.x_bf16) {
-      if (shorter) launch_direct<1, 1, 8, kBf16 | kShort>(a, l.fast, st);
-      else launch_few_rows<1, kBf16>(a, l.fast, st);
+      if (shorter) launch_direct<1, 1, 8, kBf16 | kShort>(a, st);
+      else launch_few_rows<1, kBf16>(a, st);
     } else {
-      if (shorter) launch_direct<1, 1, 8, kF32 | kShort>(a, l.fast, st);
-      else launch_few_rows<1, kF32>(a, l.fast, st);
+      if (shorter) launch_direct<1, 1, 8, kF32 | kShort>(a, st);
+      else launch_few_rows<1, kF32>(a, st);
     }
   } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect && l.c_stride * size < 1 << 24) {
     a.splits = plan.splits;
@@ -745,10 +738,10 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
     launch_tile(a, plan, l.fast, st);
   } else {
     switch (plan.rows16) {
-      case 1: launch_few_rows<1, kCodes>(a, l.fast, st); break;
-      case 2: launch_few_rows<2, kCodes>(a, l.fast, st); break;
-      case 3: launch_few_rows<3, kCodes>(a, l.fast, st); break;
-      default: launch_few_rows<4, kCodes>(a, l.fast, st);
+      case 1: launch_few_rows<1, kCodes>(a, st); break;
+      case 2: launch_few_rows<2, kCodes>(a, st); break;
+      case 3: launch_few_rows<3, kCodes>(a, st); break;
+      default: launch_few_rows<4, kCodes>(a, st);
     }
   }
   return hipGetLastError();

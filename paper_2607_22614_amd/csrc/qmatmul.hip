@@ -9,6 +9,7 @@
 
 #include <algorithm>
 
+#include "product_index.h"
 #include "quant_device.h"
 
 namespace dr {
@@ -400,20 +401,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
   const uint32_t items = items_of(p);
 
   // The copying side.  Rows [0, BM) of a stage are a's, the others b's.  What changes from tile to tile is the same for all
-  // lanes: where the tile's rows begin and how many bytes of them there are, and where their scale codes begin.  Rows
-  // past the matrix are beyond the buffer; scale codes past it are some other row's (a matrix's scales are a 128th of
-  // its data, below 2^32 bytes).
-  struct Source {
-    const uint8_t *a, *b;
-    uint32_t abytes, bbytes, acodes, bcodes, block, end;
-  };
-  auto source_of = [&](const Item& t) {
-    return Source{p.a.data + (int64_t)t.m0 * p.a.stride, p.b.data + (int64_t)t.n0 * p.b.stride,
-                  (min(t.m0 + BM, p.a.rows) - min(t.m0, p.a.rows)) * (uint32_t)p.a.stride,
-                  (min(t.n0 + BN, p.b.rows) - min(t.n0, p.b.rows)) * (uint32_t)p.b.stride,
-                  (t.m0 >> p.a.sh) * 4, (t.n0 >> p.b.sh) * 4, t.j0, t.j1};
-  };
-  Source source, upcoming;
+  // lanes (ProductSource).  Rows past the matrix are beyond the buffer; scale codes past it are some other row's (a
+  // matrix's scales are a 128th of its data, below 2^32 bytes).
+  auto source_of = [&](const Item& t) { return product_source(p.a, p.b, BM, BN, t.m0, t.n0, t.j0, t.j1); };
+  ProductSource source, upcoming;
   uint32_t from[kCopies], acode[TM], bcode[TN];
 #pragma unroll
   for (int i = 0; i < kCopies; ++i) {
@@ -435,18 +426,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     if (a_codes) copy_words_to_lds(ascales, code_at, source.acodes + source.block / 4 * p.a.srows * 4, to + kCodes + wave * 256);
     else copy_words_to_lds(bscales, code_at, source.bcodes + source.block / 4 * p.b.srows * 4, to + kCodes + wave * 256);
   };
-  // to the next block, or the first one of the upcoming item
-  auto advance = [&] {
-    const bool same = ++source.block < source.end;
-    source.a = same ? source.a : upcoming.a;
-    source.b = same ? source.b : upcoming.b;
-    source.abytes = same ? source.abytes : upcoming.abytes;
-    source.bbytes = same ? source.bbytes : upcoming.bbytes;
-    source.acodes = same ? source.acodes : upcoming.acodes;
-    source.bcodes = same ? source.bcodes : upcoming.bcodes;
-    source.block = same ? source.block : upcoming.block;
-    source.end = same ? source.end : upcoming.end;
-  };
+  auto advance = [&] { next_block(source, upcoming); };
   struct Scales {
     int a[TM], b[TN];
   };
@@ -548,12 +528,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     in = in_next;
   };
 
-  // behind the last item: nothing of its rows is there, and copies of them take no memory access
-  auto no_more = [&] { upcoming.abytes = upcoming.bbytes = 0; };
   Item t = item_of<BM, BN>(p, blockIdx.x);
   source = upcoming = source_of(t);
   if constexpr (DEEP) {
-    no_more();
+    no_product_source(upcoming);
 #pragma unroll
     for (int b = 0; b < S; ++b) {
       if (b) advance();
@@ -586,7 +564,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ProductArgs 
     const bool more = b + gridDim.x < items;
     if (more) t = item_of<BM, BN>(p, b + gridDim.x);
     upcoming = source_of(t);
-    if (!more) no_more();
+    if (!more) no_product_source(upcoming);
     if constexpr (ONE) {
       __syncthreads();  // every wave has read the block before
       now = load_scales();

@@ -583,15 +583,17 @@ enum {
  * in blocks of either kind), c is M x N of `type`, row_stride elements from row
  * to row.  The codes' products are exact and their sums are held in fp32 and
  * rounded once to `type` (bf16: ties to even).  K = 0 gives zeros (or leaves c
- * with DR_ACCUMULATE).  The sum's order depends on the shapes alone.
+ * with DR_ACCUMULATE).  The sum's order depends on the shapes alone, and on
+ * whether c's rows begin 16 MiB or more apart.
  * An element below 2^-133 counts as zero and one from 2^128 on as infinite.
  * DR_FAST_SUMS lets large products run at the rate of the 8-bit matrix
  * instructions, about twice that of the exact sums.  Within each 8 columns these
  * instructions drop what lies below 2^-13 of the largest product's power of two:
  * at most 2^-10 of sum |a||b|, and 1.5e-5 of the result's norm for normally
  * distributed values, a hundredth of what rounding to bf16 costs.  Without
- * it, and where it brings nothing (up to 32 rows of a, and other products
- * small enough to be computed the same way), sums lose no more than fp32 does.
+ * it, and where it brings nothing (up to 32 rows of a, other products
+ * small enough to be computed the same way, and rows of c that begin 16 MiB or
+ * more apart), sums lose no more than fp32 does.
  * The three products of a linear layer y = x w^T: y = (x, w); dx = dy w = (dy,
  * transpose of w); dw = dy^T x = (transpose of dy, transpose of x).
  *   c: device pointer, aligned to its type.

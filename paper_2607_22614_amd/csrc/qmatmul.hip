@@ -24,7 +24,7 @@ struct ProductArgs {
   void* c;
   int64_t c_stride;
   uint32_t m, n, kb, tiles_m, tiles_n;
-  uint32_t first, count, quarters;  // the tiles of the launch, and whether an item is a quarter of one (item_of)
+  uint32_t first, count, quarters;  // the tiles of the launch (of few rows: the first one), and whether an item is a quarter of one (item_of)
   uint32_t splits;  // of the blocks: items of one tile, whose fp32 sums go to part[split][m][part_stride]
   int64_t split_bytes;  // of c, from one split to the next (0 without them)
   int32_t c_vec, c_bf16, accumulate;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
   __shared__ f32x4 part[KS][FT * TT][64];
   const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint32_t n0 = blockIdx.x % p.tiles_n * (FT * 16), m0 = blockIdx.x / p.tiles_n * (TT * 16);
+  const uint32_t tile = p.first + blockIdx.x, n0 = tile % p.tiles_n * (FT * 16), m0 = tile / p.tiles_n * (TT * 16);
   const uint8_t *bp[FT], *ap[TT], *bcode[FT], *acode[TT];
   uint32_t arow[TT];
 #pragma unroll
@@ -230,8 +230,13 @@ __global__ __launch_bounds__(64 * KS) void product_direct_kernel(ProductArgs p) 
 template <int FT, int TT, int KS, int X>
 void launch_direct(ProductArgs a, hipStream_t st) {
   a.tiles_n = (uint32_t)ceil_div(a.n, FT * 16);
-  const dim3 grid(a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16)), block(64 * KS);
-  hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), grid, block, 0, st, a);
+  const uint32_t tiles = a.tiles_n * (uint32_t)ceil_div(a.m, TT * 16);
+  // results of tens of gigabytes are more tiles than a launch holds
+  for (a.first = 0; a.first < tiles;) {
+    const uint32_t grid = std::min(tiles - a.first, max_workgroups(64 * KS));
+    hipLaunchKernelGGL((product_direct_kernel<FT, TT, KS, X>), dim3(grid), dim3(64 * KS), 0, st, a);
+    a.first += grid;
+  }
 }
 
 // More columns a workgroup read a fewer times, fewer columns give more workgroups.  One tile of 16 columns up to 4096
@@ -311,7 +316,7 @@ __device__ __forceinline__ uint32_t bf16_pair_here(float lo, float hi) {
   return r;
 }
 
-constexpr uint32_t kOutside = 1u << 31;  // 128 rows of c lie within it (launch_product)
+constexpr uint32_t kOutside = 1u << 31;  // 128 rows of c lie within it (kMaxRowBytes)
 template <int TM, int TN, int BYTES, bool VEC>
 __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 (&acc)[TN][TM], uint8_t* lds, uint32_t m0, uint32_t n0, uint32_t lane) {
   constexpr int kXs = TN * 2 / BYTES, kPitch = TN * 64, kPiecesRow = kPitch / 16, kMask = kPiecesRow - 1, kElems = 16 / BYTES;
@@ -707,7 +712,7 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
       if (shorter) launch_direct<1, 1, 8, kF32 | kShort>(a, st);
       else launch_few_rows<1, kF32>(a, st);
     }
-  } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect && l.c_stride * size < 1 << 24) {
+  } else if (const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast); plan.kind != ProductPlan::kDirect && l.c_stride * size < kMaxRowBytes) {
     a.splits = plan.splits;
     a.split_bytes = 0;
     if (l.n * (int64_t)size % 16) a.c_vec = 0;  // whole pieces only

@@ -56,7 +56,7 @@ int check_dense(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t
   return DR_OK;
 }
 
-// The tiles of a launch are counted, and their lanes launched, in 32 bits.
+// The tiles of a product are counted in 32 bits.
 int check_results(int64_t m, int64_t n, const char* what) {
   return m * n <= 1ll << 38 ? DR_OK : fail(DR_EINVAL, "%s: %lld x %lld results (at most 2^38)", what, (long long)m, (long long)n);
 }
@@ -140,7 +140,7 @@ ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
   for (const auto kind : {ProductPlan::kTile256, ProductPlan::kTile128}) {
     const int64_t side = kind == ProductPlan::kTile256 ? 256 : 128;
     const double tiles = (double)ceil_div(m, side) * (double)ceil_div(n, side);
-    for (uint32_t splits = 1; splits <= 16 && (splits == 1 || kb >= 2 * (int64_t)splits); ++splits) {
+    for (uint32_t splits = 1; splits <= 16 && (splits == 1 || (kb >= 2 * (int64_t)splits && part_stride(n) * 4 < kMaxRowBytes)); ++splits) {
       const double steps = (double)ceil_div(kb, splits), rounds = std::ceil(tiles * splits / kCus);
       const double us = splits == 1 ? 0 : 4 + 8.0 * splits * (double)m * (double)part_stride(n) / 6.5e6;
       auto time128 = [&](double n_rounds) {

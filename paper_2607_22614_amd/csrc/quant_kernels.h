@@ -64,6 +64,13 @@ struct ProductPlan {
 inline uint32_t direct_columns16(int64_t n) { return n <= 4096 ? 1 : n <= 9216 ? 2 : 4; }
 constexpr uint32_t direct_waves(uint32_t columns16) { return columns16 == 4 ? 4 : 8; }
 
+// Workgroups of `lanes` lanes that one launch holds: it counts lanes in 32 bits.
+constexpr uint32_t max_workgroups(uint32_t lanes) { return 0xFFFFFFFFu / lanes; }
+
+// Bytes from row to row of c that the tiles can store to: the last of 128 rows begins below 2^31 bytes.  The kernel for few rows
+// takes what lies further apart.
+constexpr int64_t kMaxRowBytes = 1ll << 24;
+
 inline int64_t part_stride(int64_t n) { return ceil_div(n, 4) * 4; }
 
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast);

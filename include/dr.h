@@ -569,7 +569,7 @@ int dr_qmatrix_sizes(int64_t rows, int64_t cols, int32_t block_rows, int64_t* st
  *   src: device pointer, aligned to its element type; 16-byte aligned rows
  *   (pointer and row_stride) are read fastest.
  * Errors: DR_EINVAL (limits above, shapes that differ, row_stride < cols, null
- * or misaligned pointers, more than 2^24 tiles of 128 x 128), DR_EHIP. */
+ * or misaligned pointers, 2^23 or more tiles of 128 x 128), DR_EHIP. */
 int dr_quantize(const void* src, int32_t type, int64_t rows, int64_t cols, int64_t row_stride, const dr_qmatrix* q,
                 const dr_qmatrix* qt, void* stream);
 

@@ -67,8 +67,10 @@ int hip_result(hipError_t e, const char* what) {
 
 int quantize(const void* src, int32_t type, int64_t rows, int64_t cols, int64_t row_stride, const dr_qmatrix* q,
              const dr_qmatrix* qt, hipStream_t st, const char* what) {
-  if (ceil_div(rows, kBlock) * ceil_div(cols, kBlock) > (1 << 24))
-    return fail(DR_EINVAL, "%s: %lld x %lld is more than 2^24 tiles", what, (long long)rows, (long long)cols);
+  const int64_t tiles = ceil_div(rows, kBlock) * ceil_div(cols, kBlock);
+  if (tiles > max_workgroups(kTileLanes))
+    return fail(DR_EINVAL, "%s: %lld x %lld is %s tiles", what, (long long)rows, (long long)cols,
+                tiles > 1 << 24 ? "more than 2^24" : "2^23 or more");
   if (!rows || !cols) return DR_OK;
   QuantizeLaunch l;
   std::memset(&l, 0, sizeof(l));

@@ -34,6 +34,8 @@ struct QuantizeLaunch {
   QView q, qt;         // data null: not wanted
 };
 hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st);
+// Lanes of a workgroup that takes a tile of 128 x 128; a launch of rows alone has fewer of them in all.
+constexpr int kTileLanes = 512;
 
 // c (m x n) = a (m x k) * b^T (n x k), kb = ceil(k / 128) column blocks.
 struct ProductLaunch {

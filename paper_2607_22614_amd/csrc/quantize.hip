@@ -90,10 +90,9 @@ __device__ __forceinline__ void put_code(const QView& q, uint32_t i, uint32_t j,
 //   Tiles go in bands of four down, and 32 of them to an XCD at a time: runs of 512 to 1024 bytes of q's and qt's rows then
 // leave one L2 (8192 x 4096 fp32 both ways 43 us, in the order of the rows 45; 3000 x 3001 bf16 10.8 and 11.6).
 constexpr uint32_t kBandT = 4, kTurn = 32;
-constexpr int kTileThreads = 512;
 template <bool BF16, bool SQUARE, bool ROWS, bool COLS>
-__global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantizeArgs a) {
-  constexpr int R = 128 / (kTileThreads / 16), kWaves = kTileThreads / 64;
+__global__ __launch_bounds__(kTileLanes) void quantize_tile_kernel(QuantizeArgs a) {
+  constexpr int R = 128 / (kTileLanes / 16), kWaves = kTileLanes / 64;
   __shared__ uint32_t cmax[kWaves][128];
   __shared__ __align__(16) uint8_t turned[COLS ? 128 * 128 : 16];
   const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;
@@ -193,8 +192,8 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantizeArg
       *reinterpret_cast<uint32_t*>(turned + (tx * 8 + j) * 128 + (ty ^ (tx % 8 * 4)) * 4) = column_codes<BF16>(v, j, code[j]);
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 128 * 8 / kTileThreads; ++r) {
-      const uint32_t c = r * (kTileThreads / 8) + tid / 8, piece = tid % 8;
+    for (int r = 0; r < 128 * 8 / kTileLanes; ++r) {
+      const uint32_t c = r * (kTileLanes / 8) + tid / 8, piece = tid % 8;
       const u32x4 w = *reinterpret_cast<const u32x4*>(turned + c * 128 + (piece ^ (c / 8 % 8)) * 16);
       if (ct * 128 + c < a.cols)
         *reinterpret_cast<u32x4*>(a.qt.data + (int64_t)(ct * 128 + c) * a.qt.stride + rt * 128 + piece * 16) = w;
@@ -214,7 +213,7 @@ void launch_rows(const QuantizeArgs& a, hipStream_t st) {
 
 template <bool BF16, bool SQUARE>
 void launch_tiles(const QuantizeArgs& a, dim3 grid, hipStream_t st) {
-  const dim3 block(kTileThreads);
+  const dim3 block(kTileLanes);
   if (a.q.data && a.qt.data) {
     hipLaunchKernelGGL((quantize_tile_kernel<BF16, SQUARE, true, true>), grid, block, 0, st, a);
   } else if (a.qt.data) {

@@ -251,6 +251,15 @@ def _find_current():
     return lambda: torch.cuda.current_stream().cuda_stream
 
 
+def _forget_current():
+    global _current
+    _current = None
+
+
+# the first look initialises torch's side of the GPU, which torch refuses in a fork of a process that has used it
+os.register_at_fork(after_in_child=_forget_current)
+
+
 def _stream(stream) -> int:
     global _current
     if stream is None:

@@ -60,7 +60,7 @@ struct AnyElement<true> {
 // Elements col .. col + 7 of the row of `cols` elements at element `row` of base, aligned to the element alone.  The last 8
 // of the row stand in for those that are not all there, so that every lane loads and none branches; settle8 puts that
 // right.  A row of fewer than 8 is loaded element by element, and is right at once.
-// STREAM: rows that begin at whole 16 bytes and are read once.
+// STREAM: rows of whole 16 bytes (whole_pieces), read once.
 template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ Raw8<BF16> load_row8(const void* base, int64_t row, uint32_t col, uint32_t cols) {
   const uint8_t* p = static_cast<const uint8_t*>(base) + (row + min(col, cols - 8)) * (BF16 ? 2 : 4);

@@ -34,6 +34,10 @@ struct QuantizeLaunch {
   QView q, qt;         // data null: not wanted
 };
 hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st);
+// Whether rows begin at whole 16 bytes and consist of them, so that every load of 16 bytes of theirs is aligned.
+inline bool whole_pieces(const void* src, int64_t stride, int64_t cols, int64_t size) {
+  return reinterpret_cast<uintptr_t>(src) % 16 == 0 && stride * size % 16 == 0 && cols * size % 16 == 0;
+}
 // Lanes of a workgroup that takes a tile of 128 x 128; a launch of rows alone has fewer of them in all.
 constexpr int kTileLanes = 512;
 

@@ -22,7 +22,7 @@ struct QuantizeArgs {
 };
 
 // Eight columns of ROWS rows; rows past the matrix read its last one.  The sources of large calls are streamed past the
-// caches, where their rows begin at whole 16 bytes (those that share lines with others take 13 instead of 10 us for 3000 x
+// caches, where their rows are whole 16 bytes (those that share lines with others take 13 instead of 10 us for 3000 x
 // 3001 that way).  Of a call that moves up to kCached bytes in all the source may still lie in the last cache (256 MiB),
 // where the call that wrote it left it: 7168 x 4096 bf16 then take 14 us and streamed 16, from HBM 19 and 17; 8192 x 4096
 // both ways 28 and 25.
@@ -235,7 +235,7 @@ hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
   a.qt = l.qt;
   const int64_t size = l.bf16 ? 2 : 4;
   const int64_t moved = (int64_t)l.rows * l.cols * (size + (l.q.data != nullptr) + (l.qt.data != nullptr));
-  a.stream = moved > kCached && reinterpret_cast<uintptr_t>(l.src) % 16 == 0 && l.src_stride * size % 16 == 0;
+  a.stream = moved > kCached && whole_pieces(l.src, l.src_stride, l.cols, size);
   const bool square = (l.q.data ? l.q.sh : l.qt.sh) != 0;
   if (!square && !l.qt.data) {
     a.tiles_x = (uint32_t)ceil_div(l.cols, 512);

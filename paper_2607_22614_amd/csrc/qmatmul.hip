@@ -387,7 +387,7 @@ __device__ __forceinline__ void store_turned(const ProductArgs& p, const f32x16 
 //   S > 2: that many buffers, for workgroups that have a CU to themselves and take one item each.  The copies then run S
 // blocks ahead, and the scale codes come with them, a word (four blocks' codes) per row: loaded to registers they would have
 // to wait for the copies before them.
-//   Long products are bound by power: 8192 x 14336 x 4096 take 385 us (2500 TFLOP/s) with the matrix units busy 64 % of the
+//   Long products are bound by power: 8192 x 14336 x 4096 take 385 us (2500 TFLOP/s; 410 on a card that gets less) with the matrix units busy 64 % of the
 // cycles at a clock of about 1.8 GHz, exact sums 700 to 750 us.  Few rows are bound by how fast b comes: 61 x 151936 x 896
 // 36 us (4.7 TB/s); short K by the start and end of tiles: 768 x 9728 x 896 13 us.
 template <int BM, int BN, int WM, int WN, int BYTES, bool VEC, bool FAST, bool ONE, int S>
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256) void join_splits_kernel(ProductArgs p) {
 }
 
 // Workgroups with a CU to themselves stage four blocks, in the LDS of the second one that is not there: fast sums of 512 x
-// 6912 x 5120 in 24 us instead of 35, 100 x 32064 x 4096 37 (46), 2048 x 2000 x 2000 14 (17).  Exact sums are not faster (512 x
+// 6912 x 5120 in 24 us instead of 35 (up to 31 where less of it lies in the last cache), 100 x 32064 x 4096 37 (46), 2048 x 2000 x 2000 14 (17).  Exact sums are not faster (512 x
 // 896 x 4864 20.6 and 19.9), nor are items of two or three blocks (200 x 688 x 256 5.7 and 5.4).
 constexpr uint32_t kCus = 256;
 constexpr int kDeep = 4;

@@ -123,8 +123,9 @@ int check_workspace(const void* p, uint64_t have, uint64_t need, const char* wha
 // its steps is 8, 3 and, of two together, 4; a second launch 6; joining splits 4 and their sums' bytes, written and read, at
 // 6.5 TB/s.  A round of 256 workgroups of the kernel for few rows takes direct_step (by columns and by rows per workgroup)
 // for each 128-column block of a wave, beside direct_start and 0.5 for each further round, and no less than the weights at
-// 4.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice among tiles takes at most 14 % more than
-// the best of eight; with the kernel for few rows 64 x 2000 x 2000 6.6 instead of 11.0, 200 x 688 x 256 3.6 (5.4).
+// 4.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice takes at most 11 % more than the
+// best of eight ways with tiles and three with the kernel for few rows, in another session 19 % (200 x 4096 x 3584); that kernel
+// brings 48 x 2000 x 2000 from 10.0 to 6.7, 200 x 688 x 256 from 5.4 to 3.7.
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
   if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0, m <= 16 ? 1u : 2u};
   constexpr double kCus = 256;

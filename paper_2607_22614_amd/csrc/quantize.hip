@@ -4,8 +4,9 @@
 // element's code is x * 2^-e rounded to 4 significant bits.  Both multiplications by powers of two are
 // exact, so the codes depend on nothing but the definition.
 //
-// HBM-bound: 2 or 4 bytes read and 1 byte written per element and orientation.  8192 x 5120 bf16 along the rows take 23 us
-// (5.5 TB/s), 8192 x 4096 both ways 25 to 28 (4.8 to 5.4), 8192 x 14336 95 (5.0): a tile's codes leave only after all of it has come.
+// HBM-bound: 2 or 4 bytes read and 1 byte written per element and orientation.  8192 x 5120 bf16 along the rows take 24.5 us from
+// HBM (5.1 TB/s), fp32 42 (5.0); 8192 x 4096 both ways 29 (4.6; 25 where part of it lies in the last cache), fp32 43 (4.7); 8192 x 14336 99
+// (4.7): a tile's codes leave only after all of it has come.
 #include <hip/hip_runtime.h>
 
 #include "quant_device.h"
@@ -23,9 +24,17 @@ struct QuantizeArgs {
 
 // Eight columns of ROWS rows; rows past the matrix read its last one.  The sources of large calls are streamed past the
 // caches, where their rows are whole 16 bytes (those that share lines with others take 13 instead of 10 us for 3000 x
-// 3001 that way).  Of a call that moves up to kCached bytes in all the source may still lie in the last cache (256 MiB),
-// where the call that wrote it left it: 7168 x 4096 bf16 then take 14 us and streamed 16, from HBM 19 and 17; 8192 x 4096
-// both ways 28 and 25.
+// 3001 that way).  Streamed loads leave the last cache (256 MiB) to what the call writes, and
+// do not profit from a source that lies there.  Between calls that go round among a few sets of buffers they win where all
+// of the sets together pass the cache: from 128 MiB moved by a call with 2 sets, about 90 with 3, 64 to 72 with 4.  A
+// call does not know the others; kCached is the line for somewhat less than 3.  In us, plain / streamed:
+//                                  3 sets         from HBM       just written
+//   4096 x 4096 bf16, rows       10.6 / 11.3     12.6 / 11.0     12.5 / 12.7
+//   8192 x 4096 bf16, both ways  28.2 / 26.4     28.7 / 29.0     22.7 / 25.9
+//   16384 x 4096 bf16, rows      38.7 / 35.5
+//   8192 x 14336 bf16, rows                      66.9 / 64.7     57.5 / 61.7
+//   16384 x 4096 fp32, rows      63.1 / 60.2
+//   16384 x 4096 fp32, both ways 75.3 / 82.0, where it does not pay
 constexpr int64_t kCached = 96ll << 20;
 template <bool BF16, int ROWS>
 __device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, uint32_t col, Raw8<BF16> (&v)[ROWS]) {

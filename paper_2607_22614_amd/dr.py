@@ -16,6 +16,7 @@ addresses are passed through unchecked.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import Sequence
 
@@ -23,6 +24,18 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdr.so")
 if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2607_22614_amd.build` "
                       "(or __graft_entry__.build())")
+
+
+def _share_runtime() -> None:
+    """Loads the HIP runtime that torch brings, where it brings one, so that libdr.so takes it too whichever of the two is imported
+    first: of two runtimes in a process the second finds no device."""
+    spec = importlib.util.find_spec("torch")
+    path = os.path.join(os.path.dirname(spec.origin), "lib", "libamdhip64.so") if spec and spec.origin else ""
+    if os.path.exists(path):
+        ctypes.CDLL(path)
+
+
+_share_runtime()
 _lib = ctypes.CDLL(_LIB_PATH)
 
 DR_OK, DR_EINVAL, DR_ERANGE, DR_ENOMEM, DR_EHIP = 0, -1, -2, -3, -4

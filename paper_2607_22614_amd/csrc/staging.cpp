@@ -127,29 +127,25 @@ uint64_t chunk_out_bytes(const dr_plan* p, uint64_t chunk) {
   return chunk + 1 < p->info.num_chunks ? p->layout.chunk_bytes : p->info.last_chunk_bytes;
 }
 
-// DR_ENOMEM where the device's memory does not suffice, for a buffer or for what the runtime needs to fill it.
-int memory_result(hipError_t e, const char* call, const char* what, size_t bytes) {
-  if (e == hipSuccess) return DR_OK;
-  return fail(e == hipErrorOutOfMemory ? DR_ENOMEM : DR_EHIP, "%s(%s, %zu B): %s", call, what, bytes, hipGetErrorString(e));
-}
-
 int alloc(void** dptr, size_t bytes, const char* what) {
   bytes = std::max<size_t>(bytes, 16);
-  const hipError_t e = hipMalloc(dptr, bytes);
-  if (e != hipSuccess) *dptr = nullptr;
-  return memory_result(e, "hipMalloc", what, bytes);
+  hipError_t e = hipMalloc(dptr, bytes);
+  if (e != hipSuccess) {
+    *dptr = nullptr;
+    return fail(e == hipErrorOutOfMemory ? DR_ENOMEM : DR_EHIP, "hipMalloc(%s, %zu B): %s", what, bytes,
+                hipGetErrorString(e));
+  }
+  return DR_OK;
 }
 
-// A table that a plan keeps on its device.
-struct DeviceTable {
-  void** dptr;
-  const void* host;
-  size_t bytes;
-  const char* what;
-};
 template <typename T>
-DeviceTable device_table(T** dptr, const std::vector<T>& host, const char* what) {
-  return DeviceTable{reinterpret_cast<void**>(dptr), host.data(), host.size() * sizeof(T), what};
+int upload(T** dptr, const std::vector<T>& host, const char* what) {
+  if (int rc = alloc(reinterpret_cast<void**>(dptr), host.size() * sizeof(T), what)) return rc;
+  if (!host.empty()) {
+    const hipError_t e = hipMemcpy(*dptr, host.data(), host.size() * sizeof(T), hipMemcpyHostToDevice);
+    if (e != hipSuccess) return fail(DR_EHIP, "hipMemcpy(%s): %s", what, hipGetErrorString(e));
+  }
+  return DR_OK;
 }
 
 }  // namespace
@@ -220,25 +216,22 @@ int upload_plan(dr_plan* p) {
   hipError_t e = hipGetDevice(&p->device);
   if (e != hipSuccess) return fail(DR_EHIP, "hipGetDevice: %s", hipGetErrorString(e));
   int rc;
-  std::vector<DeviceTable> tables = {device_table(&p->d_segs, p->segs, "segments")};
-  if (!p->moment_segs.empty()) tables.push_back(device_table(&p->d_moment_segs, p->moment_segs, "moment segments"));
+  if ((rc = upload(&p->d_segs, p->segs, "segments"))) return rc;
   // per tiling: tiles, chunk index and the checksum accumulators, which start at zero (and every
   // launch leaves them at zero: ChunkSum)
+  if (!p->moment_segs.empty() && (rc = upload(&p->d_moment_segs, p->moment_segs, "moment segments"))) return rc;
   uint64_t words = 0;
   for_each_tiling(p, [&](Tiling& tl) {
-    tables.push_back(device_table(&tl.d_tiles, tl.tiles, "tiles"));
-    tables.push_back(device_table(&tl.d_chunk_tile_begin, tl.chunk_tile_begin, "chunk tiles"));
+    if (rc) return;
+    if ((rc = upload(&tl.d_tiles, tl.tiles, "tiles"))) return;
+    if ((rc = upload(&tl.d_chunk_tile_begin, tl.chunk_tile_begin, "chunk tiles"))) return;
     tl.acc0 = words;
     words += (uint64_t)(tl.chunk_tile_begin.size() - 1) * tl.sum_slots * tl.sum_stride;
   });
-  // all memory first: a plan that does not get it has copied nothing.  The runtime makes what its copies need at the
-  // process's first one, and must not have to do so in what a full device has left.
-  for (const DeviceTable& t : tables)
-    if ((rc = alloc(t.dptr, t.bytes, t.what))) return rc;
+  if (rc) return rc;
   if ((rc = alloc(reinterpret_cast<void**>(&p->d_acc), words * 8, "checksum accumulators"))) return rc;
-  for (const DeviceTable& t : tables)
-    if (t.bytes && (rc = memory_result(hipMemcpy(*t.dptr, t.host, t.bytes, hipMemcpyHostToDevice), "hipMemcpy", t.what, t.bytes))) return rc;
-  if ((rc = memory_result(hipMemset(p->d_acc, 0, words * 8), "hipMemset", "checksum accumulators", words * 8))) return rc;
+  e = hipMemset(p->d_acc, 0, words * 8);
+  if (e != hipSuccess) return fail(DR_EHIP, "hipMemset(checksum accumulators): %s", hipGetErrorString(e));
   e = hipDeviceSynchronize();
   if (e != hipSuccess) return fail(DR_EHIP, "hipDeviceSynchronize: %s", hipGetErrorString(e));
   // the static scratch of dr_stage_chunk_noalloc on this device, looked up here rather than in a call

@@ -618,6 +618,79 @@ int dr_qlinear(const void* x, int32_t x_type, int64_t m, int64_t x_row_stride, c
 int dr_qlinear_workspace(int64_t m, int64_t n, int64_t k, uint64_t* bytes);
 
 /* ---------------------------------------------------------------------------
+ * The gated feed-forward block in 8 bits, between its two linear layers, and its
+ * activation checkpoints.
+ *
+ * w holds the fused weights that the staging emits (gate_up_r): 2F x K, gate's F
+ * rows and then up's.  With gate = x w_gate^T and up = x w_up^T,
+ *   h = act(gate) * up,   act(g) = g / (1 + exp(-z)),   z = k1 g + k3 g^3:
+ *   DR_ACT_SILU       k1 = 1, k3 = 0
+ *   DR_ACT_GELU_TANH  k1 = 2 sqrt(2/pi), k3 = 0.044715 k1: 0.5 g (1 + tanh(z/2))
+ * Sums and h are held in fp32 and rounded once, where they are stored; act is
+ * off by at most (6 + |z|) 2^-23 of itself, and may be 0 where exp(-z) passes
+ * 2^126.
+ * What is saved for the backward pass is the checkpoint: x, gate and up in
+ * 8 bits (3 bytes where K = F, in place of 6 in bf16), from which the backward
+ * pass computes what it needs:
+ *   forward    dr_quantize x;  h, gate, up = dr_qgated_save(x, w);
+ *              y = dr_qmatmul(h, w_down)
+ *   backward   dr_quantize dy both ways;  dh = dr_qmatmul(dy, w_down^T);
+ *              d, d^T, h^T = dr_gated_backward(dh, gate, up);  x^T = dr_qtranspose(x);
+ *              dx = dr_qmatmul(d, w^T);  dw += dr_qmatmul(d^T, x^T);
+ *              dw_down += dr_qmatmul(dy^T, h^T)
+ */
+enum { DR_ACT_SILU = 0, DR_ACT_GELU_TANH = 1 };
+
+/* h = act(x w_gate^T) * (x w_up^T): as dr_qlinear on w (x of M x K, quantized in
+ * blocks of 1 x 128; sums and flags as there), with activation and product where
+ * the sums stand.  h is M x F of h_type.
+ *   x, h: device pointers, aligned to their types.
+ *   workspace: device buffer (16-byte aligned) of at least the bytes that
+ *   dr_qgated_workspace gives; may be NULL where that is 0.
+ * Errors: as dr_qlinear, and DR_EINVAL for w with an odd number of rows and
+ * unknown activations. */
+int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row_stride, const dr_qmatrix* w, int32_t act, void* h,
+              int32_t h_type, int64_t h_row_stride, int32_t flags, void* workspace, uint64_t workspace_bytes,
+              void* stream);
+/* f: columns of h, half of w's rows.  Errors: DR_EINVAL (null, limits above). */
+int dr_qgated_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes);
+
+/* The same in training, from x in 8 bits: h (M x F) in 8 bits, as dr_quantize
+ * gives it from the fp32 values, and so gate and up (M x F each): the
+ * checkpoint.  gate and up may both be NULL (no backward pass follows).  h, gate
+ * and up have blocks of 1 x 128, x any.
+ *   flags, workspace: as above, the bytes from dr_qgated_save_workspace.
+ * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, one of gate
+ * and up alone, null or misaligned pointers, workspace too small), DR_EHIP. */
+int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t act, const dr_qmatrix* h, const dr_qmatrix* gate,
+                   const dr_qmatrix* up, int32_t flags, void* workspace, uint64_t workspace_bytes, void* stream);
+int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes);
+
+/* The backward pass through act and the product, from the checkpoint: with dh
+ * (M x F of dh_type, dh_row_stride elements from row to row)
+ *   d  = [dgate dup] (M x 2F), dgate = dh * up * act'(gate), dup = dh * act(gate),
+ *   dt = its transpose (2F x M), and
+ *   ht = the transpose of act(gate) * up (F x M), again from the checkpoint,
+ * each in 8 bits in blocks of 1 x 128, as dr_quantize gives it from the fp32
+ * values.  Any of d, dt and ht may be NULL, but not all; F a multiple of 128 reads
+ * its inputs once, another F twice.
+ * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, null or
+ * misaligned pointers, 2^23 or more tiles of 128 x 128), DR_EHIP. */
+int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, const dr_qmatrix* gate,
+                      const dr_qmatrix* up, int32_t act, const dr_qmatrix* d, const dr_qmatrix* dt,
+                      const dr_qmatrix* ht, void* stream);
+
+/* qt = the transpose of src, quantized anew in blocks of 1 x 128 as dr_quantize
+ * would from the values that src stands for: the checkpoint x of a linear layer,
+ * turned for its weights' gradient (src in blocks of either kind).  Scales are powers
+ * of two, so an element keeps its 4 significant bits but for what lies 2^-14 and
+ * more below the largest of its new block.  Elements below 2^-133 count as zero and
+ * those from 2^128 on as NaN.
+ * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, null or
+ * misaligned pointers, 2^23 or more tiles of 128 x 128), DR_EHIP. */
+int dr_qtranspose(const dr_qmatrix* src, const dr_qmatrix* qt, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Global norm and clipping of the training role's gradients, over any number
  * of tensors: one per weight, or the W flat shards.
  *

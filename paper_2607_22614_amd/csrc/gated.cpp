@@ -1,0 +1,223 @@
+// Entry points of the gated feed-forward block (dr.h): argument checks and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "dr_internal.h"
+#include "gated_kernels.h"
+#include "quant_checks.h"
+
+namespace dr {
+namespace {
+
+int check_act(int32_t act, const char* what) {
+  return act == DR_ACT_SILU || act == DR_ACT_GELU_TANH ? DR_OK : fail(DR_EINVAL, "%s: unknown activation %d", what, act);
+}
+
+Act act_of(int32_t act) {
+  const double k1 = 2.0 * std::sqrt(2.0 / 3.14159265358979323846);
+  return act == DR_ACT_SILU ? Act{1.0f, 0.0f} : Act{(float)k1, (float)(0.044715 * k1)};
+}
+
+// An 8-bit matrix of rows x cols in blocks of 1 x 128, as activations and gradients are.
+int check_rows_matrix(const dr_qmatrix* q, int64_t rows, int64_t cols, const char* what, const char* name) {
+  if (int rc = check_matrix(q, what, name)) return rc;
+  if (q->rows != rows || q->cols != cols)
+    return fail(DR_EINVAL, "%s: %s is %lld x %lld, not %lld x %lld", what, name, (long long)q->rows, (long long)q->cols, (long long)rows, (long long)cols);
+  if (q->block_rows != 1) return fail(DR_EINVAL, "%s: %s has blocks of %d rows (1 here)", what, name, q->block_rows);
+  return DR_OK;
+}
+
+// The fused weights: gate's rows, then as many of up.
+int check_halves(const dr_qmatrix* w, const char* what) {
+  if (int rc = check_matrix(w, what, "w")) return rc;
+  return w->rows % 2 ? fail(DR_EINVAL, "%s: w has %lld rows, not gate's and as many of up", what, (long long)w->rows) : DR_OK;
+}
+
+// Where the sums of gate and up lie behind x's codes (none where codes is false or x is quantized in the product's kernel).
+struct GatedSpace {
+  uint64_t data, scales, sums, total;
+};
+GatedSpace gated_space(int64_t m, int64_t f, int64_t k, bool codes) {
+  GatedSpace s{0, 0, 0, 0};
+  if (codes && m > kFusedRows) {
+    const LinearSpace l = linear_space(m, 0, k);
+    s.data = l.data, s.scales = l.scales, s.sums = l.product;
+  }
+  uint64_t splits = 1;
+  for (bool fast : {false, true}) splits = std::max<uint64_t>(splits, plan_product(m, 2 * f, ceil_div(k, kBlock), fast).splits);
+  s.total = s.sums + splits * (uint64_t)m * part_stride(2 * f) * sizeof(float) + 16;  // the join reads whole 16 bytes
+  return s;
+}
+
+int workspace_of(int64_t m, int64_t f, int64_t k, bool codes, uint64_t* bytes, const char* what) {
+  if (!bytes) return fail(DR_EINVAL, "%s: null argument", what);
+  if (f < 0 || f > kMaxQCols) return fail(DR_EINVAL, "%s: %lld inner columns (at most 2^23)", what, (long long)f);
+  if (int rc = check_shape(m, k, 1, what, "x")) return rc;
+  if (int rc = check_shape(2 * f, k, 1, what, "w")) return rc;
+  if (int rc = check_results(m, 2 * f, what)) return rc;
+  *bytes = m && f ? gated_space(m, f, k, codes).total : 0;
+  return DR_OK;
+}
+
+// The product's sums and the join of their halves.
+int product_and_join(ProductLaunch& l, GatedJoin& j, int64_t m, int64_t f, int64_t k, const dr_qmatrix* w, uint8_t* sums, int32_t act, bool fast,
+                     hipStream_t st, const char* what) {
+  l.b = view(*w);
+  l.c = l.workspace = sums;
+  l.c_stride = part_stride(2 * f);
+  l.m = (uint32_t)m;
+  l.n = (uint32_t)(2 * f);
+  l.kb = (uint32_t)ceil_div(k, kBlock);
+  l.fast = fast;
+  l.sums = true;
+  if (int rc = hip_result(launch_product(l, st), what)) return rc;
+  j.sums = reinterpret_cast<const float*>(sums);
+  j.stride = l.c_stride;
+  j.split_stride = m * l.c_stride;
+  j.m = (uint32_t)m;
+  j.f = (uint32_t)f;
+  j.splits = plan_product(m, 2 * f, l.kb, fast).splits;
+  j.act = act_of(act);
+  return hip_result(launch_gated_join(j, st), what);
+}
+
+}  // namespace
+}  // namespace dr
+
+using namespace dr;
+
+extern "C" int dr_qgated_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
+  clear_error();
+  return workspace_of(m, f, k, true, bytes, "dr_qgated_workspace");
+}
+
+extern "C" int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
+  clear_error();
+  return workspace_of(m, f, k, false, bytes, "dr_qgated_save_workspace");
+}
+
+extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row_stride, const dr_qmatrix* w, int32_t act, void* h, int32_t h_type,
+                         int64_t h_row_stride, int32_t flags, void* workspace, uint64_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* what = "dr_qgated";
+  if (int rc = check_halves(w, what)) return rc;
+  const int64_t k = w->cols, f = w->rows / 2;
+  if (int rc = check_act(act, what)) return rc;
+  if (int rc = check_shape(m, k, 1, what, "x")) return rc;
+  if (int rc = check_dense(x, x_type, m, k, x_row_stride, what, "x")) return rc;
+  if (int rc = check_dense(h, h_type, m, f, h_row_stride, what, "h")) return rc;
+  if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
+  uint64_t need = 0;
+  if (int rc = workspace_of(m, f, k, true, &need, what)) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  if (!m || !f) return DR_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const GatedSpace s = gated_space(m, f, k, true);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  ProductLaunch l;
+  std::memset(&l, 0, sizeof(l));
+  if (m <= kFusedRows) {
+    l.x = x;
+    l.x_stride = x_row_stride;
+    l.x_bf16 = x_type == DR_TYPE_BF16;
+    l.a.cols = (uint32_t)k;
+  } else {
+    const dr_qmatrix q = {ws + s.data, ws + s.scales, m, k, padded(k), 1, 0};
+    if (int rc = quantize_checked(x, x_type, m, k, x_row_stride, &q, nullptr, st, what)) return rc;
+    l.a = view(q);
+  }
+  GatedJoin j;
+  std::memset(&j, 0, sizeof(j));
+  j.h = h;
+  j.h_stride = h_row_stride;
+  j.h_bf16 = h_type == DR_TYPE_BF16;
+  return product_and_join(l, j, m, f, k, w, ws + s.sums, act, (flags & DR_FAST_SUMS) != 0, st, what);
+}
+
+extern "C" int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t act, const dr_qmatrix* h, const dr_qmatrix* gate, const dr_qmatrix* up,
+                              int32_t flags, void* workspace, uint64_t workspace_bytes, void* stream) {
+  clear_error();
+  const char* what = "dr_qgated_save";
+  if (int rc = check_matrix(x, what, "x")) return rc;
+  if (int rc = check_halves(w, what)) return rc;
+  const int64_t m = x->rows, k = w->cols, f = w->rows / 2;
+  if (x->cols != k) return fail(DR_EINVAL, "%s: x has %lld columns, w %lld", what, (long long)x->cols, (long long)k);
+  if (int rc = check_act(act, what)) return rc;
+  if (int rc = check_rows_matrix(h, m, f, what, "h")) return rc;
+  if (!gate != !up) return fail(DR_EINVAL, "%s: one of gate and up without the other", what);
+  if (gate) {
+    if (int rc = check_rows_matrix(gate, m, f, what, "gate")) return rc;
+    if (int rc = check_rows_matrix(up, m, f, what, "up")) return rc;
+  }
+  if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
+  uint64_t need = 0;
+  if (int rc = workspace_of(m, f, k, false, &need, what)) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  if (!m || !f) return DR_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  ProductLaunch l;
+  std::memset(&l, 0, sizeof(l));
+  l.a = view(*x);
+  GatedJoin j;
+  std::memset(&j, 0, sizeof(j));
+  j.hq = view(*h);
+  if (gate) {
+    j.gate = view(*gate);
+    j.up = view(*up);
+  }
+  return product_and_join(l, j, m, f, k, w, static_cast<uint8_t*>(workspace), act, (flags & DR_FAST_SUMS) != 0, st, what);
+}
+
+extern "C" int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, const dr_qmatrix* gate, const dr_qmatrix* up, int32_t act,
+                                 const dr_qmatrix* d, const dr_qmatrix* dt, const dr_qmatrix* ht, void* stream) {
+  clear_error();
+  const char* what = "dr_gated_backward";
+  if (int rc = check_matrix(gate, what, "gate")) return rc;
+  const int64_t m = gate->rows, f = gate->cols;
+  if (int rc = check_rows_matrix(gate, m, f, what, "gate")) return rc;
+  if (int rc = check_rows_matrix(up, m, f, what, "up")) return rc;
+  if (int rc = check_act(act, what)) return rc;
+  if (int rc = check_dense(dh, dh_type, m, f, dh_row_stride, what, "dh")) return rc;
+  if (!d && !dt && !ht) return fail(DR_EINVAL, "%s: none of d, dt and ht given", what);
+  if (d) {
+    if (int rc = check_rows_matrix(d, m, 2 * f, what, "d")) return rc;
+  }
+  if (dt) {
+    if (int rc = check_rows_matrix(dt, 2 * f, m, what, "dt")) return rc;
+  }
+  if (ht) {
+    if (int rc = check_rows_matrix(ht, f, m, what, "ht")) return rc;
+  }
+  const int64_t tiles = backward_tiles_x(f) * ceil_div(m, kBlock);
+  if (tiles > max_workgroups(kTileLanes)) return fail(DR_EINVAL, "%s: %lld x %lld is 2^23 or more tiles", what, (long long)m, (long long)f);
+  if (!m || !f) return DR_OK;
+  GatedBackward l;
+  std::memset(&l, 0, sizeof(l));
+  l.dh = dh;
+  l.dh_stride = dh_row_stride;
+  l.dh_bf16 = dh_type == DR_TYPE_BF16;
+  l.rows = (uint32_t)m;
+  l.f = (uint32_t)f;
+  l.act = act_of(act);
+  l.gate = view(*gate);
+  l.up = view(*up);
+  if (d) l.d = view(*d);
+  if (dt) l.dt = view(*dt);
+  if (ht) l.ht = view(*ht);
+  return hip_result(launch_gated_backward(l, static_cast<hipStream_t>(stream)), what);
+}
+
+extern "C" int dr_qtranspose(const dr_qmatrix* src, const dr_qmatrix* qt, void* stream) {
+  clear_error();
+  const char* what = "dr_qtranspose";
+  if (int rc = check_matrix(src, what, "src")) return rc;
+  if (int rc = check_rows_matrix(qt, src->cols, src->rows, what, "qt")) return rc;
+  const int64_t tiles = ceil_div(src->rows, kBlock) * ceil_div(src->cols, kBlock);
+  if (tiles > max_workgroups(kTileLanes))
+    return fail(DR_EINVAL, "%s: %lld x %lld is 2^23 or more tiles", what, (long long)src->rows, (long long)src->cols);
+  if (!src->rows || !src->cols) return DR_OK;
+  return hip_result(launch_turn(view(*src), view(*qt), static_cast<hipStream_t>(stream)), what);
+}

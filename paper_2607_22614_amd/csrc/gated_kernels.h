@@ -1,0 +1,46 @@
+// Launches of the gated feed-forward kernels (gated.hip, gated_backward.hip): plain arguments, checked by the host code that
+// fills them (gated.cpp).  Each wrapper enqueues on `st` and returns hipGetLastError().
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "quant_kernels.h"
+
+namespace dr {
+
+// act(g) = g / (1 + exp(-z)) with z = g (k1 + k3 g^2): silu with k1 = 1, k3 = 0; the tanh form of gelu, 0.5 g (1 + tanh(z / 2)),
+// with k1 = 2 sqrt(2 / pi), k3 = 0.044715 k1.
+struct Act {
+  float k1, k3;
+};
+
+// h = act(gate) * up where a product's sums hold gate in columns [0, f) and up in [f, 2f): `splits` parts, split_stride
+// elements apart, are added in their order.  Readable are 4 elements behind the last part.
+struct GatedJoin {
+  const float* sums;
+  int64_t stride, split_stride;  // elements
+  uint32_t m, f, splits;
+  Act act;
+  void* h;           // set: rows of bf16 or fp32
+  int64_t h_stride;  // elements
+  bool h_bf16;
+  QView hq, gate, up;  // h null: 8 bits; gate and up: data null: not wanted
+};
+hipError_t launch_gated_join(const GatedJoin& l, hipStream_t st);
+
+// d = [dgate dup] and its transpose, and h^T, from dh and the checkpoint; data null: not wanted.
+struct GatedBackward {
+  const void* dh;
+  int64_t dh_stride;  // elements
+  bool dh_bf16;
+  uint32_t rows, f;
+  Act act;
+  QView gate, up, d, dt, ht;
+};
+hipError_t launch_gated_backward(const GatedBackward& l, hipStream_t st);
+// Columns of tiles that launch_gated_backward takes.
+inline int64_t backward_tiles_x(int64_t f) { return f % kBlock ? ceil_div(2 * f, kBlock) : f / kBlock; }
+
+}  // namespace dr

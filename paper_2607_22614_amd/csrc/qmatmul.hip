@@ -669,8 +669,9 @@ void launch_tile_kind(const ProductArgs& a, const ProductPlan& plan, bool fast, 
   }
 }
 
-void launch_tile(const ProductArgs& a, const ProductPlan& plan, bool fast, hipStream_t st) {
-  if (a.splits == 1) {
+// sums: the splits' sums stay in the workspace, unjoined, those of a single one too.
+void launch_tile(const ProductArgs& a, const ProductPlan& plan, bool fast, bool sums, hipStream_t st) {
+  if (a.splits == 1 && !sums) {
     if (a.c_bf16) launch_tile_kind<2>(a, plan, fast, st);
     else launch_tile_kind<4>(a, plan, fast, st);
     return;
@@ -683,6 +684,7 @@ void launch_tile(const ProductArgs& a, const ProductPlan& plan, bool fast, hipSt
   parts.n = (uint32_t)a.part_stride;  // columns past b's last one: sums of zeros
   parts.accumulate = 0;
   launch_tile_kind<4>(parts, plan, fast, st);
+  if (sums) return;
   hipLaunchKernelGGL(join_splits_kernel, dim3((uint32_t)std::min<int64_t>(2048, ceil_div(a.m * (a.part_stride / 4), 256))), dim3(256), 0, st, a);
 }
 
@@ -718,7 +720,7 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
     if (l.n * (int64_t)size % 16) a.c_vec = 0;  // whole pieces only
     a.part = static_cast<float*>(l.workspace);
     a.part_stride = part_stride(l.n);
-    launch_tile(a, plan, l.fast, st);
+    launch_tile(a, plan, l.fast, l.sums, st);
   } else {
     switch (plan.rows16) {
       case 1: launch_few_rows<1, kCodes>(a, st); break;

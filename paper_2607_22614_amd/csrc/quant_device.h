@@ -184,6 +184,18 @@ __device__ __forceinline__ uint32_t column_codes(const Raw8<BF16> (&v)[4], int j
   return to_e4m3_f32(bits_of<BF16>(v[0], j), bits_of<BF16>(v[1], j), bits_of<BF16>(v[2], j), bits_of<BF16>(v[3], j), s);
 }
 
+// What 8 codes and their scale stand for, in bf16 (exact: 4 significant bits; below 2^-133 it is 0).
+__device__ __forceinline__ Raw8<true> bf16_values(u32x2 codes, uint32_t code) {
+  const float s = scale_operand(code);
+  Raw8<true> v;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v.w[0][2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes[i], s, false));
+    v.w[0][2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes[i], s, true));
+  }
+  return v;
+}
+
 // fp32 -> bf16, ties to even (the hardware convert).
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});

@@ -34,6 +34,8 @@ struct QuantizeLaunch {
   QView q, qt;         // data null: not wanted
 };
 hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st);
+// qt = the transpose of src, both in 8 bits.
+hipError_t launch_turn(const QView& src, const QView& qt, hipStream_t st);
 // Whether rows begin at whole 16 bytes and consist of them, so that every load of 16 bytes of theirs is aligned.
 inline bool whole_pieces(const void* src, int64_t stride, int64_t cols, int64_t size) {
   return reinterpret_cast<uintptr_t>(src) % 16 == 0 && stride * size % 16 == 0 && cols * size % 16 == 0;
@@ -51,6 +53,7 @@ struct ProductLaunch {
   int64_t c_stride;  // elements
   uint32_t m, n, kb;
   bool c_bf16, accumulate, fast;
+  bool sums;         // c is fp32 rows of part_stride(n) in the workspace: what each of the plan's splits sums goes there, m rows a split
   void* workspace;
 };
 hipError_t launch_product(const ProductLaunch& l, hipStream_t st);

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include "quant_device.h"
+#include "quantize_tile.h"
 
 namespace dr {
 namespace {
@@ -82,132 +83,46 @@ __global__ __launch_bounds__(64 * kRowWaves) void quantize_rows_kernel(QuantizeA
     reinterpret_cast<uint32_t*>(a.q.scales)[(int64_t)quad * a.rows + row0 + lane] = word;
 }
 
-// Scale code of block (i, j) of a matrix with R block rows, and 127 in the unused bytes of its last word.
-__device__ __forceinline__ void put_code(const QView& q, uint32_t i, uint32_t j, uint32_t code) {
-  const uint32_t blocks = (q.cols + 127) / 128;
-  uint8_t* p = q.scales + ((int64_t)(j >> 2) * q.srows + i) * 4;
-  p[j & 3] = (uint8_t)code;
-  if (j + 1 == blocks)
-    for (uint32_t k = (j & 3) + 1; k < 4; ++k) p[k] = 127;
-}
-
 // A tile of 128 x 128 per workgroup, each lane 8 columns of 4 rows, kept in registers (of 8 rows by half the lanes: 200 x 256
-// bf16 both ways 5.0 us instead of 4.5, 2000 x 4096 fp32 14.1 and 13.4).  ROWS writes the codes along the rows, COLS the
-// transpose: its codes are packed 4 rows to a word, turned in LDS (one 128-byte row per column, its words spread by an
-// exclusive or over the banks), and leave as whole 128-byte rows.  SQUARE: one scale for the tile, else one per row (DPP) and
-// one per column (over the four rows of lanes, then over the waves in LDS).
-//   Tiles go in bands of four down, and 32 of them to an XCD at a time: runs of 512 to 1024 bytes of q's and qt's rows then
-// leave one L2 (8192 x 4096 fp32 both ways 43 us, in the order of the rows 45; 3000 x 3001 bf16 10.8 and 11.6).
-constexpr uint32_t kBandT = 4, kTurn = 32;
+// bf16 both ways 5.0 us instead of 4.5, 2000 x 4096 fp32 14.1 and 13.4).
 template <bool BF16, bool SQUARE, bool ROWS, bool COLS>
 __global__ __launch_bounds__(kTileLanes) void quantize_tile_kernel(QuantizeArgs a) {
-  constexpr int R = 128 / (kTileLanes / 16), kWaves = kTileLanes / 64;
-  __shared__ uint32_t cmax[kWaves][128];
-  __shared__ __align__(16) uint8_t turned[COLS ? 128 * 128 : 16];
-  const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;
-  const uint32_t t = xcd_group<kTurn>(blockIdx.x, gridDim.x), tiles_y = gridDim.x / a.tiles_x, band = t / (kBandT * a.tiles_x);
-  const uint32_t high = min(kBandT, tiles_y - band * kBandT), i_band = t - band * kBandT * a.tiles_x;
-  const uint32_t rt = band * kBandT + i_band % high, ct = i_band / high;
-  const uint32_t col = ct * 128 + tx * 8, row0 = rt * 128 + ty * R;
-  Raw8<BF16> v[R];
-  load_rows(a, row0, col, v);
-  if (row0 + R > a.rows) {
+  __shared__ TileSpace<COLS> space;
+  const TilePlace at = tile_place(a.tiles_x);
+  Raw8<BF16> v[kTileRows];
+  load_rows(a, at.row0, at.col, v);
+  if (at.row0 + kTileRows > a.rows) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (row0 + i >= a.rows) v[i] = Raw8<BF16>{};
+    for (int i = 0; i < kTileRows; ++i)
+      if (at.row0 + i >= a.rows) v[i] = Raw8<BF16>{};
   }
-  // the lane's largest magnitude of each row; finite ones only if any is not
-  uint32_t rmax[R], top = 0;
-#pragma unroll
-  for (int i = 0; i < R; ++i) top = max(top, rmax[i] = row_max(v[i], false));
-  const bool odd = __any(top >= kInfBits);
-  if (odd) {
-    top = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) top = max(top, rmax[i] = row_max(v[i], true));
-  }
+  quantize_tile<BF16, SQUARE, ROWS, COLS>(v, at, a.q, a.qt, space);
+}
 
-  uint32_t square_code = 0;
-  if (SQUARE) {
-    const uint32_t m = max_rows(max16(top));
-    if ((tid & 63) == 0) cmax[0][wave] = m;
-    __syncthreads();
-    uint32_t most = cmax[0][0];
+// The transpose of an 8-bit matrix, quantized anew.  The values go through bf16, which holds them: 4 significant bits, and
+// what lies below 2^-133 counts as 0 as in the products.
+struct TurnArgs {
+  QView src, qt;
+  uint32_t tiles_x;
+};
+__global__ __launch_bounds__(kTileLanes) void turn_tile_kernel(TurnArgs a) {
+  __shared__ TileSpace<true> space;
+  const TilePlace at = tile_place(a.tiles_x);
+  Raw8<true> v[kTileRows];
+  u32x2 codes[kTileRows];
+  uint32_t scale[kTileRows];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) most = max(most, cmax[0][w]);
-    square_code = scale_code(most);
-    if (tid == 0) {
-      if (ROWS) put_code(a.q, rt, ct, square_code);
-      if (COLS) put_code(a.qt, ct, rt, square_code);
-    }
+  for (int i = 0; i < kTileRows; ++i) {
+    const uint32_t row = min(at.row0 + i, a.src.rows - 1);
+    codes[i] = *reinterpret_cast<const u32x2*>(a.src.data + (int64_t)row * a.src.stride + at.col);
+    scale[i] = a.src.scales[((int64_t)(at.ct >> 2) * a.src.srows + (row >> a.src.sh)) * 4 + (at.ct & 3)];
   }
-
-  if (ROWS) {
-    uint32_t mine = 0;  // of row row0 + tx
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const uint32_t code = SQUARE ? square_code : scale_code(max16(rmax[i]));
-      mine = tx == (uint32_t)i ? code : mine;
-      if (row0 + i < a.rows)
-        *reinterpret_cast<u32x2*>(a.q.data + (int64_t)(row0 + i) * a.q.stride + col) = row_codes(v[i], code);
-    }
-    if (!SQUARE && tx < R && row0 + tx < a.rows) put_code(a.q, row0 + tx, ct, mine);
+  for (int i = 0; i < kTileRows; ++i) {
+    v[i] = bf16_values(codes[i], scale[i]);
+    if (at.row0 + i >= a.src.rows) v[i] = Raw8<true>{};
   }
-
-  if (COLS) {
-    uint32_t code[8], mine = 0;  // of column col + ty
-    if (SQUARE) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) code[j] = square_code;
-    } else {
-      uint32_t most[BF16 ? 4 : 8] = {};
-      auto column_max = [&](bool finite) {
-#pragma unroll
-        for (int w = 0; w < (BF16 ? 4 : 8); ++w)
-#pragma unroll
-          for (int i = 0; i < R; ++i) most[w] = larger<BF16>(most[w], magnitude<BF16>(v[i].w[BF16 ? 0 : w / 4][w % 4], finite));
-      };
-      if (odd) column_max(true);
-      else column_max(false);
-#pragma unroll
-      for (int w = 0; w < (BF16 ? 4 : 8); ++w) {
-        uint32_t m = most[w];
-        m = larger<BF16>(m, (uint32_t)__shfl_xor((int)m, 16));
-        m = larger<BF16>(m, (uint32_t)__shfl_xor((int)m, 32));
-        if ((tid & 63) < 16) {
-          if (BF16) {
-            cmax[wave][tx * 8 + 2 * w] = m << 16;
-            cmax[wave][tx * 8 + 2 * w + 1] = m & 0xFFFF0000u;
-          } else {
-            cmax[wave][tx * 8 + w] = m;
-          }
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t c = tx * 8 + j;
-        uint32_t m = cmax[0][c];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = max(m, cmax[w][c]);
-        code[j] = scale_code(m);
-        mine = ty == (uint32_t)j ? code[j] : mine;
-      }
-      if (ty < 8 && col + ty < a.cols) put_code(a.qt, col + ty, rt, mine);
-    }
-    // word ty of a column lies at ty ^ 4 (tx % 8), which keeps its 16-byte pieces together
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<uint32_t*>(turned + (tx * 8 + j) * 128 + (ty ^ (tx % 8 * 4)) * 4) = column_codes<BF16>(v, j, code[j]);
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 128 * 8 / kTileLanes; ++r) {
-      const uint32_t c = r * (kTileLanes / 8) + tid / 8, piece = tid % 8;
-      const u32x4 w = *reinterpret_cast<const u32x4*>(turned + c * 128 + (piece ^ (c / 8 % 8)) * 16);
-      if (ct * 128 + c < a.cols)
-        *reinterpret_cast<u32x4*>(a.qt.data + (int64_t)(ct * 128 + c) * a.qt.stride + rt * 128 + piece * 16) = w;
-    }
-  }
+  quantize_tile<true, false, false, true>(v, at, QView{}, a.qt, space);
 }
 
 // Eight rows a wave keep the loads of a long matrix in flight; where that leaves CUs without work, one.
@@ -261,6 +176,12 @@ hipError_t launch_quantize(const QuantizeLaunch& l, hipStream_t st) {
     if (square) launch_tiles<false, true>(a, grid, st);
     else launch_tiles<false, false>(a, grid, st);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_turn(const QView& src, const QView& qt, hipStream_t st) {
+  const uint32_t tiles_x = (uint32_t)ceil_div(src.cols, 128);
+  hipLaunchKernelGGL(turn_tile_kernel, dim3(tiles_x * (uint32_t)ceil_div(src.rows, 128)), dim3(kTileLanes), 0, st, TurnArgs{src, qt, tiles_x});
   return hipGetLastError();
 }
 

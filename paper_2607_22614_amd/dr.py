@@ -115,6 +115,7 @@ class dr_grad(ctypes.Structure):
 DR_TYPE_F32, DR_TYPE_BF16 = 0, 1
 DR_QUANT_BLOCK = 128
 DR_ACCUMULATE, DR_FAST_SUMS = 1, 2
+DR_ACT_SILU, DR_ACT_GELU_TANH = 0, 1
 DR_HYST_BALANCED, DR_HYST_PERSISTENCE, DR_HYST_COOLDOWN, DR_HYST_DWELL, DR_HYST_EDGE, DR_HYST_AMORTIZE, \
     DR_HYST_RESIZE = range(7)
 
@@ -156,6 +157,14 @@ _SIGS = {
     "dr_qlinear": ([_P, ctypes.c_int32, _I64, _I64, _PQ, _P, ctypes.c_int32, _I64, ctypes.c_int32, _P,
                     ctypes.c_uint64, _P], ctypes.c_int),
     "dr_qlinear_workspace": ([_I64, _I64, _I64, _PU64], ctypes.c_int),
+    "dr_qgated": ([_P, ctypes.c_int32, _I64, _I64, _PQ, ctypes.c_int32, _P, ctypes.c_int32, _I64, ctypes.c_int32, _P,
+                   ctypes.c_uint64, _P], ctypes.c_int),
+    "dr_qgated_workspace": ([_I64, _I64, _I64, _PU64], ctypes.c_int),
+    "dr_qgated_save": ([_PQ, _PQ, ctypes.c_int32, _PQ, _PQ, _PQ, ctypes.c_int32, _P, ctypes.c_uint64, _P],
+                       ctypes.c_int),
+    "dr_qgated_save_workspace": ([_I64, _I64, _I64, _PU64], ctypes.c_int),
+    "dr_gated_backward": ([_P, ctypes.c_int32, _I64, _PQ, _PQ, ctypes.c_int32, _PQ, _PQ, _PQ, _P], ctypes.c_int),
+    "dr_qtranspose": ([_PQ, _PQ, _P], ctypes.c_int),
     "dr_grad_workspace": ([_PU64], ctypes.c_int),
     "dr_grad_norm": ([ctypes.POINTER(dr_grad), _I64, _P, _P, _P, _P], ctypes.c_int),
     "dr_grad_scale": ([ctypes.POINTER(dr_grad), _I64, _P, ctypes.c_double, _P, _P], ctypes.c_int),
@@ -683,6 +692,65 @@ def dr_qlinear(x, w: QMatrix, out, fast: bool = False, workspace=None, stream=No
 def dr_qlinear_workspace(m: int, w: QMatrix) -> int:
     """Bytes of workspace that dr_qlinear needs for m rows and these weights."""
     return _bytes(_lib.dr_qlinear_workspace, "dr_qlinear_workspace", int(m), w.rows, w.cols)
+
+
+# ------------------------------------------------------------------ the gated feed-forward block
+def _on_current(where: str, *tensors) -> None:
+    """The calls run on the current device: a tensor of another one is refused (None and the like are skipped)."""
+    import torch
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"{where}: a tensor on {t.device}, the current device is {current}")
+
+
+def dr_qgated(x, w: QMatrix, out, act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
+    """out = act(x w_gate^T) * (x w_up^T) with w = [w_gate; w_up] and x (2-d float32 or bfloat16) quantized in blocks of
+    1 x 128; fast: DR_FAST_SUMS."""
+    addr, kind, rows, cols, step = _dense_rows(x, "dr_qgated x")
+    oaddr, okind, orows, ocols, ostep = _dense_rows(out, "dr_qgated out")
+    if cols != w.cols or orows != rows or 2 * ocols != w.rows:
+        raise ValueError(f"dr_qgated: x {rows} x {cols}, w {w.rows} x {w.cols}, out {orows} x {ocols}")
+    _on_current("dr_qgated", x, w.data, out, workspace)
+    _check(_lib.dr_qgated(addr, kind, rows, step, w.ref, act, oaddr, okind, ostep, DR_FAST_SUMS if fast else 0,
+                          *_workspace(workspace, "dr_qgated workspace"), _stream(stream)), "dr_qgated")
+
+
+def dr_qgated_workspace(m: int, w: QMatrix) -> int:
+    """Bytes of workspace that dr_qgated needs for m rows and these weights."""
+    return _bytes(_lib.dr_qgated_workspace, "dr_qgated_workspace", int(m), w.rows // 2, w.cols)
+
+
+def dr_qgated_save(x: QMatrix, w: QMatrix, h: QMatrix, gate: QMatrix | None = None, up: QMatrix | None = None,
+                   act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
+    """h = act(x w_gate^T) * (x w_up^T) in 8 bits, and the halves of x w^T as the checkpoint for dr_gated_backward;
+    fast: DR_FAST_SUMS."""
+    _on_current("dr_qgated_save", x.data, w.data, h.data, gate and gate.data, up and up.data, workspace)
+    _check(_lib.dr_qgated_save(x.ref, w.ref, act, h.ref, gate and gate.ref, up and up.ref, DR_FAST_SUMS if fast else 0,
+                               *_workspace(workspace, "dr_qgated_save workspace"), _stream(stream)), "dr_qgated_save")
+
+
+def dr_qgated_save_workspace(m: int, w: QMatrix) -> int:
+    """Bytes of workspace that dr_qgated_save needs for m rows and these weights."""
+    return _bytes(_lib.dr_qgated_save_workspace, "dr_qgated_save_workspace", int(m), w.rows // 2, w.cols)
+
+
+def dr_gated_backward(dh, gate: QMatrix, up: QMatrix, d: QMatrix | None = None, dt: QMatrix | None = None,
+                      ht: QMatrix | None = None, act: int = DR_ACT_SILU, stream=None) -> None:
+    """From dh (2-d float32 or bfloat16) and the checkpoint: d = [dgate dup], its transpose dt, and ht, the transpose of
+    act(gate) * up."""
+    addr, kind, rows, cols, step = _dense_rows(dh, "dr_gated_backward dh")
+    if rows != gate.rows or cols != gate.cols:
+        raise ValueError(f"dr_gated_backward: dh {rows} x {cols}, gate {gate.rows} x {gate.cols}")
+    _on_current("dr_gated_backward", dh, gate.data, up.data, d and d.data, dt and dt.data, ht and ht.data)
+    _check(_lib.dr_gated_backward(addr, kind, step, gate.ref, up.ref, act, d and d.ref, dt and dt.ref, ht and ht.ref,
+                                  _stream(stream)), "dr_gated_backward")
+
+
+def dr_qtranspose(src: QMatrix, qt: QMatrix, stream=None) -> None:
+    """qt = the transpose of src, quantized anew in blocks of 1 x 128."""
+    _on_current("dr_qtranspose", src.data, qt.data)
+    _check(_lib.dr_qtranspose(src.ref, qt.ref, _stream(stream)), "dr_qtranspose")
 
 
 # ------------------------------------------------------------------ gradients

@@ -36,67 +36,104 @@ int check_halves(const dr_qmatrix* w, const char* what) {
   return w->rows % 2 ? fail(DR_EINVAL, "%s: w has %lld rows, not gate's and as many of up", what, (long long)w->rows) : DR_OK;
 }
 
-// Where the sums of gate and up lie behind x's codes (none where codes is false or x is quantized in the product's kernel).
+// Where x's codes lie in the workspace of dr_qgated (none where x is quantized in the product's kernel), and behind them the
+// sums of gate and up where a product's splits have to be joined.
 struct GatedSpace {
   uint64_t data, scales, sums, total;
 };
-GatedSpace gated_space(int64_t m, int64_t f, int64_t k, bool codes) {
+uint64_t sums_space(int64_t m, int64_t f, uint32_t splits) {
+  return splits * (uint64_t)m * part_stride(2 * f) * sizeof(float) + 16;  // the join reads whole 16 bytes
+}
+GatedSpace gated_space(int64_t m, int64_t f, int64_t k) {
   GatedSpace s{0, 0, 0, 0};
-  if (codes && m > kFusedRows) {
+  if (m > kFusedRows) {
     const LinearSpace l = linear_space(m, 0, k);
-    s.data = l.data, s.scales = l.scales, s.sums = l.product;
+    s.data = l.data, s.scales = l.scales, s.total = s.sums = l.product;
   }
-  uint64_t splits = 1;
-  for (bool fast : {false, true}) splits = std::max<uint64_t>(splits, plan_product(m, 2 * f, ceil_div(k, kBlock), fast).splits);
-  s.total = s.sums + splits * (uint64_t)m * part_stride(2 * f) * sizeof(float) + 16;  // the join reads whole 16 bytes
+  for (bool fast : {false, true}) {
+    const uint32_t splits = plan_product(m, 2 * f, ceil_div(k, kBlock), fast).splits;
+    if (splits > 1) s.total = std::max(s.total, s.sums + sums_space(m, f, splits));
+  }
   return s;
 }
+uint64_t save_space(int64_t m, int64_t f, int64_t k) {
+  uint64_t total = 0;
+  const int64_t kb = ceil_div(k, kBlock);
+  for (bool fast : {false, true})
+    if (!plan_gated_codes(m, f, kb, fast).rows) total = std::max(total, sums_space(m, f, plan_product(m, 2 * f, kb, fast).splits));
+  return total;
+}
 
-int workspace_of(int64_t m, int64_t f, int64_t k, bool codes, uint64_t* bytes, const char* what) {
+int workspace_of(int64_t m, int64_t f, int64_t k, bool save, uint64_t* bytes, const char* what) {
   if (!bytes) return fail(DR_EINVAL, "%s: null argument", what);
   if (f < 0 || f > kMaxQCols) return fail(DR_EINVAL, "%s: %lld inner columns (at most 2^23)", what, (long long)f);
   if (int rc = check_shape(m, k, 1, what, "x")) return rc;
   if (int rc = check_shape(2 * f, k, 1, what, "w")) return rc;
   if (int rc = check_results(m, 2 * f, what)) return rc;
-  *bytes = m && f ? gated_space(m, f, k, codes).total : 0;
+  *bytes = !m || !f ? 0 : save ? save_space(m, f, k) : gated_space(m, f, k).total;
   return DR_OK;
 }
 
-// The product's sums and the join of their halves.
-int product_and_join(ProductLaunch& l, GatedJoin& j, int64_t m, int64_t f, int64_t k, const dr_qmatrix* w, uint8_t* sums, int32_t act, bool fast,
-                     hipStream_t st, const char* what) {
-  l.b = view(*w);
-  l.c = l.workspace = sums;
-  l.c_stride = part_stride(2 * f);
+ProductLaunch product_with(const dr_qmatrix& w, int64_t m, bool fast) {
+  ProductLaunch l;
+  std::memset(&l, 0, sizeof(l));
+  l.b = view(w);
   l.m = (uint32_t)m;
-  l.n = (uint32_t)(2 * f);
-  l.kb = (uint32_t)ceil_div(k, kBlock);
+  l.n = (uint32_t)w.rows;
+  l.kb = (uint32_t)ceil_div(w.cols, kBlock);
   l.fast = fast;
+  return l;
+}
+
+// The product's sums, and the join of their halves into what j holds.
+int product_and_join(ProductLaunch l, GatedJoin& j, uint8_t* sums, Act act, hipStream_t st, const char* what) {
+  l.c = l.workspace = sums;
+  l.c_stride = part_stride(l.n);
+  l.c_bf16 = false;
   l.sums = true;
   if (int rc = hip_result(launch_product(l, st), what)) return rc;
   j.sums = reinterpret_cast<const float*>(sums);
   j.stride = l.c_stride;
-  j.split_stride = m * l.c_stride;
-  j.m = (uint32_t)m;
-  j.f = (uint32_t)f;
-  j.splits = plan_product(m, 2 * f, l.kb, fast).splits;
-  j.act = act_of(act);
+  j.split_stride = l.m * l.c_stride;
+  j.m = l.m;
+  j.f = l.n / 2;
+  j.splits = plan_product(l.m, l.n, l.kb, l.fast).splits;
+  j.act = act;
   return hip_result(launch_gated_join(j, st), what);
 }
 
 }  // namespace
+
+GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast) {
+  const ProductPlan sums = plan_product(m, 2 * f, kb, fast);
+  if (sums.kind == ProductPlan::kDirect && m <= 32) return {0, 0};
+  constexpr double kCus = 256;
+  const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.85 : 1.5, start256 = 12, start128 = 7;
+  GatedCodesPlan best{0, 0};
+  double least = sums.us + 4 + 20.0 * sums.splits * (double)m * (double)f / 6.5e6;
+  auto consider = [&](double us, GatedCodesPlan plan) {
+    if (us < least) least = us, best = plan;
+  };
+  const double columns = (double)ceil_div(f, 128), lone = (double)kb * step128 + start128, round = (double)kb * step256 + start256;
+  consider(std::ceil(columns * (double)ceil_div(m, 128) / kCus) * lone, {128, 0});
+  if (kb < 2) return best;
+  const double tiles = columns * (double)ceil_div(m, 256), rounds = std::ceil(tiles / kCus), rest = tiles - kCus * (rounds - 1);
+  consider(rounds * round, {256, 0});
+  if (rounds > 1 && rest < kCus) consider((rounds - 1) * round + 6 + std::ceil(2 * rest / kCus) * lone, {256, (uint32_t)rest});
+  return best;
+}
 }  // namespace dr
 
 using namespace dr;
 
 extern "C" int dr_qgated_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
   clear_error();
-  return workspace_of(m, f, k, true, bytes, "dr_qgated_workspace");
+  return workspace_of(m, f, k, false, bytes, "dr_qgated_workspace");
 }
 
 extern "C" int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
   clear_error();
-  return workspace_of(m, f, k, false, bytes, "dr_qgated_save_workspace");
+  return workspace_of(m, f, k, true, bytes, "dr_qgated_save_workspace");
 }
 
 extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row_stride, const dr_qmatrix* w, int32_t act, void* h, int32_t h_type,
@@ -111,14 +148,13 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
   if (int rc = check_dense(h, h_type, m, f, h_row_stride, what, "h")) return rc;
   if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
   uint64_t need = 0;
-  if (int rc = workspace_of(m, f, k, true, &need, what)) return rc;
+  if (int rc = workspace_of(m, f, k, false, &need, what)) return rc;
   if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
   if (!m || !f) return DR_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const GatedSpace s = gated_space(m, f, k, true);
+  const GatedSpace s = gated_space(m, f, k);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  ProductLaunch l;
-  std::memset(&l, 0, sizeof(l));
+  ProductLaunch l = product_with(*w, m, (flags & DR_FAST_SUMS) != 0);
   if (m <= kFusedRows) {
     l.x = x;
     l.x_stride = x_row_stride;
@@ -129,12 +165,22 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
     if (int rc = quantize_checked(x, x_type, m, k, x_row_stride, &q, nullptr, st, what)) return rc;
     l.a = view(q);
   }
+  l.c = h;
+  l.c_stride = h_row_stride;
+  l.c_bf16 = h_type == DR_TYPE_BF16;
+  if (plan_product(m, 2 * f, l.kb, l.fast).splits == 1) {
+    GatedProduct g;
+    std::memset(&g, 0, sizeof(g));
+    g.product = l;
+    g.act = act_of(act);
+    return hip_result(launch_gated_rows(g, st), what);
+  }
   GatedJoin j;
   std::memset(&j, 0, sizeof(j));
   j.h = h;
   j.h_stride = h_row_stride;
   j.h_bf16 = h_type == DR_TYPE_BF16;
-  return product_and_join(l, j, m, f, k, w, ws + s.sums, act, (flags & DR_FAST_SUMS) != 0, st, what);
+  return product_and_join(l, j, ws + s.sums, act_of(act), st, what);
 }
 
 extern "C" int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t act, const dr_qmatrix* h, const dr_qmatrix* gate, const dr_qmatrix* up,
@@ -154,13 +200,24 @@ extern "C" int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t 
   }
   if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
   uint64_t need = 0;
-  if (int rc = workspace_of(m, f, k, false, &need, what)) return rc;
+  if (int rc = workspace_of(m, f, k, true, &need, what)) return rc;
   if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
   if (!m || !f) return DR_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProductLaunch l;
-  std::memset(&l, 0, sizeof(l));
+  ProductLaunch l = product_with(*w, m, (flags & DR_FAST_SUMS) != 0);
   l.a = view(*x);
+  if (const GatedCodesPlan plan = plan_gated_codes(m, f, l.kb, l.fast); plan.rows) {
+    GatedProduct g;
+    std::memset(&g, 0, sizeof(g));
+    g.product = l;
+    g.act = act_of(act);
+    g.hq = view(*h);
+    if (gate) {
+      g.gate = view(*gate);
+      g.up = view(*up);
+    }
+    return hip_result(launch_gated_codes(g, plan, st), what);
+  }
   GatedJoin j;
   std::memset(&j, 0, sizeof(j));
   j.hq = view(*h);
@@ -168,7 +225,7 @@ extern "C" int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t 
     j.gate = view(*gate);
     j.up = view(*up);
   }
-  return product_and_join(l, j, m, f, k, w, static_cast<uint8_t*>(workspace), act, (flags & DR_FAST_SUMS) != 0, st, what);
+  return product_and_join(l, j, static_cast<uint8_t*>(workspace), act_of(act), st, what);
 }
 
 extern "C" int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, const dr_qmatrix* gate, const dr_qmatrix* up, int32_t act,

@@ -16,6 +16,22 @@ struct Act {
   float k1, k3;
 };
 
+// The product with the fused weights (b: gate's rows, then up's; n: all of them), with act(gate) * up in place of its sums.
+struct GatedProduct {
+  ProductLaunch product;
+  Act act;
+  QView hq, gate, up;  // of launch_gated_codes; gate and up: data null: not wanted
+};
+// Into rows of c, m x n / 2, by the plan of the m x n product, which has no splits.
+hipError_t launch_gated_rows(const GatedProduct& g, hipStream_t st);
+// Into 8 bits: tiles of 256 or 128 rows by 128 columns, of which the last `halved` ones of 256 rows are cut into two each.
+//   rows 0: as a product of fp32 sums and their join.
+struct GatedCodesPlan {
+  uint32_t rows, halved;
+};
+GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast);
+hipError_t launch_gated_codes(const GatedProduct& g, const GatedCodesPlan& plan, hipStream_t st);
+
 // h = act(gate) * up where a product's sums hold gate in columns [0, f) and up in [f, 2f): `splits` parts, split_stride
 // elements apart, are added in their order.  Readable are 4 elements behind the last part.
 struct GatedJoin {

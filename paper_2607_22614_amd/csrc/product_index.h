@@ -17,6 +17,7 @@ namespace dr {
 struct ProductSource {
   const uint8_t *a, *b;
   uint32_t abytes, bbytes, acodes, bcodes, block, end;
+  uint32_t bfirst;  // row of b
 };
 
 // Rows of an operand that a tile of `tile` rows from row `at` on reads.
@@ -32,7 +33,7 @@ __host__ __device__ __forceinline__ ProductSource product_source(const QView& a,
                                                                  uint32_t n0, uint32_t j0, uint32_t j1) {
   const StagedRows m = staged_rows(m0, tile_m, a.rows), n = staged_rows(n0, tile_n, b.rows);
   return ProductSource{a.data + (int64_t)m.first * a.stride, b.data + (int64_t)n.first * b.stride, m.count * (uint32_t)a.stride,
-                       n.count * (uint32_t)b.stride, (m.first >> a.sh) * 4, (n.first >> b.sh) * 4, j0, j1};
+                       n.count * (uint32_t)b.stride, (m.first >> a.sh) * 4, (n.first >> b.sh) * 4, j0, j1, n.first};
 }
 
 // Behind the last item: copies of nothing, which take no memory access.
@@ -47,6 +48,7 @@ __host__ __device__ __forceinline__ void next_block(ProductSource& s, const Prod
   s.bbytes = same ? s.bbytes : upcoming.bbytes;
   s.acodes = same ? s.acodes : upcoming.acodes;
   s.bcodes = same ? s.bcodes : upcoming.bcodes;
+  s.bfirst = same ? s.bfirst : upcoming.bfirst;
   s.block = same ? s.block : upcoming.block;
   s.end = same ? s.end : upcoming.end;
 }

@@ -59,10 +59,10 @@ LinearSpace linear_space(int64_t m, int64_t n, int64_t k) {
 // best of eight ways with tiles and three with the kernel for few rows, in another session 19 % (200 x 4096 x 3584); that kernel
 // brings 48 x 2000 x 2000 from 10.0 to 6.7, 200 x 688 x 256 from 5.4 to 3.7.
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
-  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0, m <= 16 ? 1u : 2u};
+  if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0, m <= 16 ? 1u : 2u, 0};
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.63 : 0.78, pair128 = fast ? 0.96 : 1.72;
-  ProductPlan best{ProductPlan::kTile256, 1, 0, 2};
+  ProductPlan best{ProductPlan::kTile256, 1, 0, 2, 0};
   double least = HUGE_VAL;
   constexpr double direct_step[3][3] = {{1.45, 1.72, 2.45}, {1.88, 2.3, 2.9}, {1.35, 1.75, 2.1}}, direct_start[3] = {1.8, 3, 3};
   const uint32_t columns16 = direct_columns16(n), waves = direct_waves(columns16), wide = columns16 / 2;
@@ -70,7 +70,7 @@ ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
   for (uint32_t rows16 = 2; rows16 <= 4; ++rows16) {
     const double rounds = std::ceil((double)ceil_div(n, 16 * columns16) * (double)ceil_div(m, 16 * rows16) / kCus);
     const double us = std::max(direct_start[wide] + rounds * blocks * direct_step[wide][rows16 - 2] + 0.5 * (rounds - 1), 2 + 128.0 * (double)kb * (double)n / 4.5e6);
-    if (us < least) least = us, best = {ProductPlan::kDirect, 1, 0, rows16};
+    if (us < least) least = us, best = {ProductPlan::kDirect, 1, 0, rows16, us};
   }
   for (const auto kind : {ProductPlan::kTile256, ProductPlan::kTile128}) {
     const int64_t side = kind == ProductPlan::kTile256 ? 256 : 128;
@@ -84,7 +84,7 @@ ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
         return pairs * (steps * pair128 + 4) + lone * (steps * step + 3);
       };
       auto consider = [&](double time, uint32_t quartered) {
-        if (us + time < least) least = us + time, best = {kind, splits, quartered, 2};
+        if (us + time < least) least = us + time, best = {kind, splits, quartered, 2, us + time};
       };
       if (kind == ProductPlan::kTile128) {
         consider(time128(rounds), 0);

@@ -68,6 +68,7 @@ struct ProductPlan {
   uint32_t splits;
   uint32_t quartered;
   uint32_t rows16;  // of kDirect: 1 to 4
+  double us;        // what it should take; 0 up to 32 rows
 };
 // Tiles of 16 columns per workgroup of the kernel for few rows, and its waves, by the columns of c.
 inline uint32_t direct_columns16(int64_t n) { return n <= 4096 ? 1 : n <= 9216 ? 2 : 4; }

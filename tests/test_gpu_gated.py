@@ -234,3 +234,80 @@ def test_replayed_graph_on_another_stream(m):
         torch.cuda.synchronize()
         for a, b in zip(want, [out] + [t for q in saved for t in (q.data, q.scales)]):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def _want_large(xv, wv, kind, fast):
+    """_want with the products on the GPU, in 64 bits.  Fast sums lose 2^-10 of sum |x||w| at most."""
+    xg, wg = torch.from_numpy(xv).cuda(), torch.from_numpy(wv).cuda()
+    y, size = (xg @ wg.t()).cpu().numpy(), (xg.abs() @ wg.abs().t()).cpu().numpy()
+    f = wv.shape[0] // 2
+    d = ((-(-xv.shape[1] // 128) * 128 + 64) * 2.0**-23 + (2.0**-10 if fast else 0.0)) * size
+    gate, up, dg, du = y[:, :f], y[:, f:], d[:, :f], d[:, f:]
+    a, _, z = gated.act(gate, kind)
+    h = a * up
+    tol = 1.13 * dg * (np.abs(up) + du) + np.abs(a) * du + (8 + np.minimum(np.abs(z), 150)) * 2.0**-23 * np.abs(h) + 2.0**-117 * (np.abs(up) + du)
+    return (gate, up, h), (dg, du, tol)
+
+
+def _large_inputs(dr, m, f, k, seed, block_rows):
+    """Quantized on the GPU (dr_quantize is tested apart), and what the codes stand for."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((m, k), generator=gen, device="cuda") * torch.exp2(torch.randint(-2, 3, (m, 1), generator=gen, device="cuda").float())
+    w = torch.randn((2 * f, k), generator=gen, device="cuda") * (2.0 / k**0.5)
+    xq, wq = dr.QMatrix.empty(m, k), dr.QMatrix.empty(2 * f, k, block_rows)
+    dr.dr_quantize(x, xq), dr.dr_quantize(w, wq)
+    values = [quant.values(q.data.cpu().numpy(), q.scales.cpu().numpy(), k, b) for q, b in ((xq, 1), (wq, block_rows))]
+    return x, xq, wq, *values
+
+
+# tiles of 256 rows and of 128, last rounds of them cut in two or four, tiles alone on their CU, and splits; columns that
+# are no multiple of a tile or of 16 bytes
+LARGE = [(1157, 8100, 300), (2050, 8200, 640), (520, 4104, 1000), (1000, 700, 2176), (3000, 3456, 256), (130, 2000, 2000), (257, 6001, 129), (700, 9000, 128)]
+
+
+@pytest.mark.parametrize("m,f,k", LARGE)
+@pytest.mark.parametrize("fast", [True, False])
+@pytest.mark.parametrize("block_rows", [128, 1])
+def test_large(m, f, k, fast, block_rows):
+    dr = _dr()
+    kind = GELU if fast else SILU
+    x, xq, wq, xv, wv = _large_inputs(dr, m, f, k, m + f, block_rows)
+    (gate, up, h), (dg, du, tol) = _want_large(xv, wv, kind, fast)
+    say("large gated", m, f, k, fast, block_rows)
+    for out_type in (torch.bfloat16, torch.float32):
+        out = torch.full((m + 1, f), 7.0, dtype=out_type, device="cuda")
+        dr.dr_qgated(x, wq, out[:m], act=kind, fast=fast, workspace=_space(dr, m, wq))
+        torch.cuda.synchronize()
+        _close(out[:m], h, tol, out_type == torch.bfloat16)
+        assert (out[m] == 7.0).all()
+    say("large save", m, f, k, fast, block_rows)
+    made = [poisoned(dr, m, f) for _ in range(3)]
+    dr.dr_qgated_save(xq, wq, *(q for q, _, _ in made), act=kind, fast=fast, workspace=_space(dr, m, wq, save=True))
+    torch.cuda.synchronize()
+    for one, want, t, name in zip(made, (h, gate, up), (tol, dg, du), ("h", "gate", "up")):
+        check_rows(one, want, t, name)
+
+
+def test_large_not_finite():
+    """A row of x that is not finite, and gates past fp32's range, in the tiles of a long batch."""
+    dr = _dr()
+    say("large, not finite")
+    m, f, k = 600, 4200, 512
+    x, xq, wq, xv, wv = _large_inputs(dr, m, f, k, 1, 128)
+    xq.data[77, 5] = 0x7F
+    xv[77] = np.nan
+    xq.scales[:, 300] = 254  # 2^127 times the codes: infinite sums of either sign
+    (gate, up, h), (dg, du, tol) = _want_large(xv, wv, SILU, False)
+    skip = np.zeros(m, dtype=bool)
+    skip[300] = True
+    made = [poisoned(dr, m, f) for _ in range(3)]
+    dr.dr_qgated_save(xq, wq, *(q for q, _, _ in made), workspace=_space(dr, m, wq, save=True))
+    torch.cuda.synchronize()
+    codes = [q.data[300, :f].cpu().numpy() & 0x7F for q, _, _ in made]
+    assert all((c == 0x7F).mean() > 0.9 for c in codes[1:])  # nearly all sums are infinite
+    for one, want, t, name in zip(made, (h, gate, up), (tol, dg, du), ("h", "gate", "up")):
+        q, wide, scales = one
+        q.data[300] = q.data[299]
+        q.scales[:, 300] = q.scales[:, 299]
+        want[300], t[300] = want[299], t[299]
+        check_rows(one, want, np.where(np.isnan(t), 0.0, t), name)

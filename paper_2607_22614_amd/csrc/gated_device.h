@@ -8,11 +8,13 @@
 
 namespace dr {
 
+constexpr float kMinusLog2e = -1.44269504088896340736f;
+
 // z of act, times -log2(e).  g is cut off at 128, where the logistic function is 0 or 1 in fp32 for either activation: an infinite
 // g or g^2 would make 0 * inf in z.
 __device__ __forceinline__ float exponent(float g, const Act& act) {
   const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
-  return c * fmaf(c * c, act.k3, act.k1) * -1.44269504088896340736f;
+  return c * fmaf(c * c, act.k3, act.k1) * kMinusLog2e;
 }
 
 // The exponent is rounded to fp32, so the logistic function is off by (6 + |z|) 2^-23 of itself at most, and it is 0 where e^-z
@@ -21,15 +23,19 @@ __device__ __forceinline__ float gated(float gate, float up, const Act& act) {
   return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(exponent(gate, act))) * up;
 }
 
-struct GatedGradient {
-  float dgate, dup, h;
+// act, and act' = s + g s (1 - s) z'.  1 - s is off by 2^-23 at most, and so the slope by |z| 2^-21.  SILU: k1 = 1, k3 = 0, at half the
+// instructions.
+struct ActSlope {
+  float act, slope;
 };
-// act' = s + g s (1 - s) z', where 1 - s = e^-z s loses nothing to cancellation; the exponent is cut off at 126, past which s is
-// 0, so that no infinity meets it.
-__device__ __forceinline__ GatedGradient gated_gradient(float dh, float gate, float up, const Act& act) {
-  const float x = exponent(gate, act), e = __builtin_amdgcn_exp2f(fminf(x, 126.0f)), s = x > 126.0f ? 0.0f : __builtin_amdgcn_rcpf(1.0f + e);
-  const float c = __builtin_amdgcn_fmed3f(gate, -128.0f, 128.0f), slope = fmaf(c * c, 3.0f * act.k3, act.k1), a = gate * s;
-  return GatedGradient{dh * up * fmaf(a * slope, e * s, s), dh * a, a * up};
+template <bool SILU>
+__device__ __forceinline__ ActSlope act_slope(float g, const Act& act) {
+  if (SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * kMinusLog2e)), a = g * s;
+    return ActSlope{a, fmaf(a, 1.0f - s, s)};
+  }
+  const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(exponent(g, act))), a = g * s, c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
+  return ActSlope{a, fmaf(a * fmaf(c * c, 3.0f * act.k3, act.k1), 1.0f - s, s)};
 }
 
 __device__ __forceinline__ float element(const Raw8<false>& v, int i) { return __uint_as_float(bits_of<false>(v, i)); }

@@ -16,6 +16,7 @@
 #include "gated_device.h"
 #include "product_index.h"
 #include "quant_device.h"
+#include "quantize_values.h"
 
 namespace dr {
 namespace {
@@ -441,9 +442,6 @@ __device__ __forceinline__ float here(float v) {
   asm volatile("" : "+v"(v));
   return v;
 }
-
-// |v|, or NaN where v is not finite: the maximum passes over NaN.
-__device__ __forceinline__ float finite_magnitude(float v) { return fmaf(v, 0.0f, fabsf(v)); }
 
 // Results of a wave in 8 bits: of TM * 32 rows, TN / 2 * 32 columns of gate, up and h each, half a block of 128.  A row's largest
 // magnitudes go to the wave beside it, which has the block's other half, through the waves' own LDS (`mine` and `other`,

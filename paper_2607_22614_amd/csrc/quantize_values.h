@@ -1,0 +1,147 @@
+// Quantization along rows and columns of a tile of 128 x 128 fp32 values that a workgroup has computed: what quantize_tile does
+// (quantize_tile.h), where the vector units and not the memory would be the bound.
+//
+// Maxima go through v_max3 on magnitudes, which passes over NaN; infinities are looked for in the result, and only where there
+// are any are all maxima taken again.  A scale is carried as amax's bits + 0x1FFFFF: less 8 << 23 (or 0) it is the converts'
+// operand, whose exponent alone counts, and its own exponent less 8 the scale's code.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "quantize_tile.h"
+
+namespace dr {
+
+// A lane's values: 8 columns of kTileRows rows.
+struct TileValues {
+  float v[kTileRows][8];
+};
+
+struct ValuesSpace {
+  __align__(16) uint32_t cmax[3][128];  // of up to three matrices, zero at the start
+  __align__(16) uint8_t turned[128 * 128];
+};
+// The workgroup's first barrier has to follow.
+__device__ __forceinline__ void clear_maxima(ValuesSpace& space) {
+  if (threadIdx.x < 3 * 128 / 4) reinterpret_cast<u32x4*>(space.cmax)[threadIdx.x] = u32x4{};
+}
+
+constexpr uint32_t kRoundUp = 0x1FFFFF, kEight = 8u << 23;
+__device__ __forceinline__ uint32_t biased_scale(uint32_t amax) { return amax + kRoundUp; }
+__device__ __forceinline__ float biased_operand(uint32_t b) { return __uint_as_float(__builtin_elementwise_sub_sat(b, kEight)); }
+__device__ __forceinline__ uint32_t biased_code(uint32_t b) { return b == kRoundUp ? 127u : __builtin_elementwise_sub_sat(b, kEight) >> 23; }
+
+// |v|, or NaN where v is not finite.
+__device__ __forceinline__ float finite_magnitude(float v) { return fmaf(v, 0.0f, fabsf(v)); }
+template <bool FINITE>
+__device__ __forceinline__ float magnitude_of(float v) {
+  return FINITE ? finite_magnitude(v) : fabsf(v);
+}
+__device__ __forceinline__ uint32_t max_bits(float a, uint32_t b) { return max(__float_as_uint(a), b); }
+
+template <bool FINITE>
+__device__ __forceinline__ void row_maxima(const TileValues& t, float (&most)[kTileRows]) {
+#pragma unroll
+  for (int i = 0; i < kTileRows; ++i) {
+    float m = magnitude_of<FINITE>(t.v[i][0]);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) m = fmaxf(m, magnitude_of<FINITE>(t.v[i][j]));
+    most[i] = fmaxf(m, 0.0f);  // NaN alone counts as nothing
+  }
+}
+template <bool FINITE>
+__device__ __forceinline__ void column_maxima(const TileValues& t, float (&most)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float m = magnitude_of<FINITE>(t.v[0][j]);
+#pragma unroll
+    for (int i = 1; i < kTileRows; ++i) m = fmaxf(m, magnitude_of<FINITE>(t.v[i][j]));
+    most[j] = fmaxf(m, 0.0f);
+  }
+}
+
+__device__ __forceinline__ void put_rows(const TileValues& t, const TilePlace& at, const QView& q) {
+  const uint32_t tx = threadIdx.x & 15;
+  float most[kTileRows];
+  row_maxima<false>(t, most);
+  float top = most[0];
+#pragma unroll
+  for (int i = 1; i < kTileRows; ++i) top = fmaxf(top, most[i]);
+  if (__any(__float_as_uint(top) >= kInfBits)) row_maxima<true>(t, most);
+  uint32_t mine = 0;  // of row row0 + tx
+#pragma unroll
+  for (int i = 0; i < kTileRows; ++i) {
+    const uint32_t b = biased_scale(max16(__float_as_uint(most[i])));
+    const float s = biased_operand(b);
+    mine = tx == (uint32_t)i ? b : mine;
+    const float* v = t.v[i];
+    if (at.row0 + i < q.rows)
+      *reinterpret_cast<u32x2*>(q.data + (int64_t)(at.row0 + i) * q.stride + at.col) =
+          u32x2{to_e4m3_f32(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]), s),
+                to_e4m3_f32(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]), s)};
+  }
+  if (tx < kTileRows && at.row0 + tx < q.rows) put_code(q, at.row0 + tx, at.ct, biased_code(mine));
+}
+
+// Two registers' maxima over the lanes 32 (or 16) apart, in one: of a in the lower lanes, of b in the upper ones.
+__device__ __forceinline__ float max_halves(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_row_pairs(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// `which` of the space's maxima are this matrix's, still zero.
+__device__ __forceinline__ void put_columns(const TileValues& t, const TilePlace& at, const QView& qt, ValuesSpace& space, int which) {
+  const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, line = ty & 3;
+  float most[8];
+  column_maxima<false>(t, most);
+  float top = most[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) top = fmaxf(top, most[j]);
+  if (__any(__float_as_uint(top) >= kInfBits)) column_maxima<true>(t, most);
+  // over the wave's four rows of lanes: columns j and j + 4 meet in a register, lower and upper lanes, then j and j + 2
+  float pair[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pair[j] = max_halves(most[j], most[j + 4]);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float m = max_row_pairs(pair[j], pair[j + 2]);  // of column j, j + 2, j + 4, j + 6 in lines 0 to 3
+    atomicMax(&space.cmax[which][tx * 8 + j + line * 2], __float_as_uint(m));
+  }
+  __syncthreads();
+  uint32_t b[8], mine = 0;  // of column col + ty
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(&space.cmax[which][tx * 8 + h * 4]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[h * 4 + j] = biased_scale(w[j]);
+  }
+  // word ty of a column lies at ty ^ 4 (tx % 8), which keeps its 16-byte pieces together
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    mine = ty == (uint32_t)j ? b[j] : mine;
+    *reinterpret_cast<uint32_t*>(space.turned + (tx * 8 + j) * 128 + (ty ^ (tx % 8 * 4)) * 4) =
+        to_e4m3_f32(__float_as_uint(t.v[0][j]), __float_as_uint(t.v[1][j]), __float_as_uint(t.v[2][j]), __float_as_uint(t.v[3][j]), biased_operand(b[j]));
+  }
+  if (ty < 8 && at.col + ty < qt.rows) put_code(qt, at.col + ty, at.rt, biased_code(mine));
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 128 * 8 / kTileLanes; ++r) {
+    const uint32_t c = r * (kTileLanes / 8) + tid / 8, piece = tid % 8;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(space.turned + c * 128 + (piece ^ (c / 8 % 8)) * 16);
+    if (at.ct * 128 + c < qt.rows)
+      *reinterpret_cast<u32x4*>(qt.data + (int64_t)(at.ct * 128 + c) * qt.stride + at.rt * 128 + piece * 16) = w;
+  }
+}
+
+// The tile's codes along the rows into q, along the columns into qt, whichever are wanted.  A following call's writes of the
+// turned codes stand behind the barrier of its maxima, and so behind this one's reads.
+__device__ __forceinline__ void put_tile(const TileValues& t, const TilePlace& at, const QView& q, const QView& qt, ValuesSpace& space, int which) {
+  if (q.data) put_rows(t, at, q);
+  if (qt.data) put_columns(t, at, qt, space, which);
+}
+
+}  // namespace dr

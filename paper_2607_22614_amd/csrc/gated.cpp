@@ -39,38 +39,34 @@ int check_halves(const dr_qmatrix* w, const char* what) {
 // Where x's codes lie in the workspace of dr_qgated (none where x is quantized in the product's kernel), and behind them the
 // sums of gate and up where a product's splits have to be joined.
 struct GatedSpace {
-  uint64_t data, scales, sums, total;
+  uint64_t data, scales, sums;
 };
+GatedSpace gated_space(int64_t m, int64_t k) {
+  if (m <= kFusedRows) return {0, 0, 0};
+  const uint64_t scales = (uint64_t)m * padded(k);
+  return {0, scales, (scales + (uint64_t)ceil_div(padded(k) / kBlock, 4) * m * 4 + 15) / 16 * 16};
+}
 uint64_t sums_space(int64_t m, int64_t f, uint32_t splits) {
   return splits * (uint64_t)m * part_stride(2 * f) * sizeof(float) + 16;  // the join reads whole 16 bytes
 }
-GatedSpace gated_space(int64_t m, int64_t f, int64_t k) {
-  GatedSpace s{0, 0, 0, 0};
-  if (m > kFusedRows) {
-    const LinearSpace l = linear_space(m, 0, k);
-    s.data = l.data, s.scales = l.scales, s.total = s.sums = l.product;
-  }
-  for (bool fast : {false, true}) {
-    const uint32_t splits = plan_product(m, 2 * f, ceil_div(k, kBlock), fast).splits;
-    if (splits > 1) s.total = std::max(s.total, s.sums + sums_space(m, f, splits));
-  }
-  return s;
+uint64_t rows_need(int64_t m, int64_t f, int64_t k, const ProductPlan& plan) {
+  return gated_space(m, k).sums + (plan.splits > 1 ? sums_space(m, f, plan.splits) : 0);
 }
-uint64_t save_space(int64_t m, int64_t f, int64_t k) {
-  uint64_t total = 0;
-  const int64_t kb = ceil_div(k, kBlock);
-  for (bool fast : {false, true})
-    if (!plan_gated_codes(m, f, kb, fast).rows) total = std::max(total, sums_space(m, f, plan_product(m, 2 * f, kb, fast).splits));
-  return total;
-}
+uint64_t save_need(int64_t m, int64_t f, const GatedCodesPlan& plan) { return plan.rows ? 0 : sums_space(m, f, plan.sums.splits); }
 
-int workspace_of(int64_t m, int64_t f, int64_t k, bool save, uint64_t* bytes, const char* what) {
-  if (!bytes) return fail(DR_EINVAL, "%s: null argument", what);
+int check_sizes(int64_t m, int64_t f, int64_t k, const char* what) {
   if (f < 0 || f > kMaxQCols) return fail(DR_EINVAL, "%s: %lld inner columns (at most 2^23)", what, (long long)f);
   if (int rc = check_shape(m, k, 1, what, "x")) return rc;
   if (int rc = check_shape(2 * f, k, 1, what, "w")) return rc;
-  if (int rc = check_results(m, 2 * f, what)) return rc;
-  *bytes = !m || !f ? 0 : save ? save_space(m, f, k) : gated_space(m, f, k).total;
+  return check_results(m, 2 * f, what);
+}
+
+// What either kind of sums needs, whichever the caller asks for.
+template <class Need>
+int workspace_of(int64_t m, int64_t f, int64_t k, uint64_t* bytes, const char* what, Need need) {
+  if (!bytes) return fail(DR_EINVAL, "%s: null argument", what);
+  if (int rc = check_sizes(m, f, k, what)) return rc;
+  *bytes = m && f ? std::max(need(false), need(true)) : 0;
   return DR_OK;
 }
 
@@ -97,7 +93,7 @@ int product_and_join(ProductLaunch l, GatedJoin& j, uint8_t* sums, Act act, hipS
   j.split_stride = l.m * l.c_stride;
   j.m = l.m;
   j.f = l.n / 2;
-  j.splits = plan_product(l.m, l.n, l.kb, l.fast).splits;
+  j.splits = l.plan->splits;
   j.act = act;
   return hip_result(launch_gated_join(j, st), what);
 }
@@ -106,20 +102,20 @@ int product_and_join(ProductLaunch l, GatedJoin& j, uint8_t* sums, Act act, hipS
 
 GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast) {
   const ProductPlan sums = plan_product(m, 2 * f, kb, fast);
-  if (sums.kind == ProductPlan::kDirect && m <= 32) return {0, 0};
+  if (m <= 32 || !kb) return {0, 0, sums};
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.85 : 1.5, start256 = 12, start128 = 7;
-  GatedCodesPlan best{0, 0};
+  GatedCodesPlan best{0, 0, sums};
   double least = sums.us + 4 + 20.0 * sums.splits * (double)m * (double)f / 6.5e6;
   auto consider = [&](double us, GatedCodesPlan plan) {
     if (us < least) least = us, best = plan;
   };
   const double columns = (double)ceil_div(f, 128), lone = (double)kb * step128 + start128, round = (double)kb * step256 + start256;
-  consider(std::ceil(columns * (double)ceil_div(m, 128) / kCus) * lone, {128, 0});
+  consider(std::ceil(columns * (double)ceil_div(m, 128) / kCus) * lone, {128, 0, sums});
   if (kb < 2) return best;
   const double tiles = columns * (double)ceil_div(m, 256), rounds = std::ceil(tiles / kCus), rest = tiles - kCus * (rounds - 1);
-  consider(rounds * round, {256, 0});
-  if (rounds > 1 && rest < kCus) consider((rounds - 1) * round + 6 + std::ceil(2 * rest / kCus) * lone, {256, (uint32_t)rest});
+  consider(rounds * round, {256, 0, sums});
+  if (rounds > 1 && rest < kCus) consider((rounds - 1) * round + 6 + std::ceil(2 * rest / kCus) * lone, {256, (uint32_t)rest, sums});
   return best;
 }
 }  // namespace dr
@@ -128,12 +124,14 @@ using namespace dr;
 
 extern "C" int dr_qgated_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
   clear_error();
-  return workspace_of(m, f, k, false, bytes, "dr_qgated_workspace");
+  return workspace_of(m, f, k, bytes, "dr_qgated_workspace",
+                      [=](bool fast) { return rows_need(m, f, k, plan_product(m, 2 * f, ceil_div(k, kBlock), fast)); });
 }
 
 extern "C" int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
   clear_error();
-  return workspace_of(m, f, k, true, bytes, "dr_qgated_save_workspace");
+  return workspace_of(m, f, k, bytes, "dr_qgated_save_workspace",
+                      [=](bool fast) { return save_need(m, f, plan_gated_codes(m, f, ceil_div(k, kBlock), fast)); });
 }
 
 extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row_stride, const dr_qmatrix* w, int32_t act, void* h, int32_t h_type,
@@ -147,14 +145,15 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
   if (int rc = check_dense(x, x_type, m, k, x_row_stride, what, "x")) return rc;
   if (int rc = check_dense(h, h_type, m, f, h_row_stride, what, "h")) return rc;
   if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
-  uint64_t need = 0;
-  if (int rc = workspace_of(m, f, k, false, &need, what)) return rc;
-  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  if (int rc = check_sizes(m, f, k, what)) return rc;
   if (!m || !f) return DR_OK;
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  const GatedSpace s = gated_space(m, f, k);
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
   ProductLaunch l = product_with(*w, m, (flags & DR_FAST_SUMS) != 0);
+  const ProductPlan plan = plan_product(m, 2 * f, l.kb, l.fast);
+  if (int rc = check_workspace(workspace, workspace_bytes, rows_need(m, f, k, plan), what)) return rc;
+  l.plan = &plan;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const GatedSpace s = gated_space(m, k);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
   if (m <= kFusedRows) {
     l.x = x;
     l.x_stride = x_row_stride;
@@ -168,7 +167,7 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
   l.c = h;
   l.c_stride = h_row_stride;
   l.c_bf16 = h_type == DR_TYPE_BF16;
-  if (plan_product(m, 2 * f, l.kb, l.fast).splits == 1) {
+  if (plan.splits == 1) {
     GatedProduct g;
     std::memset(&g, 0, sizeof(g));
     g.product = l;
@@ -199,14 +198,15 @@ extern "C" int dr_qgated_save(const dr_qmatrix* x, const dr_qmatrix* w, int32_t 
     if (int rc = check_rows_matrix(up, m, f, what, "up")) return rc;
   }
   if (flags & ~DR_FAST_SUMS) return fail(DR_EINVAL, "%s: unknown flags %d", what, flags);
-  uint64_t need = 0;
-  if (int rc = workspace_of(m, f, k, true, &need, what)) return rc;
-  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  if (int rc = check_sizes(m, f, k, what)) return rc;
   if (!m || !f) return DR_OK;
-  hipStream_t st = static_cast<hipStream_t>(stream);
   ProductLaunch l = product_with(*w, m, (flags & DR_FAST_SUMS) != 0);
+  const GatedCodesPlan plan = plan_gated_codes(m, f, l.kb, l.fast);
+  if (int rc = check_workspace(workspace, workspace_bytes, save_need(m, f, plan), what)) return rc;
+  l.plan = &plan.sums;
+  hipStream_t st = static_cast<hipStream_t>(stream);
   l.a = view(*x);
-  if (const GatedCodesPlan plan = plan_gated_codes(m, f, l.kb, l.fast); plan.rows) {
+  if (plan.rows) {
     GatedProduct g;
     std::memset(&g, 0, sizeof(g));
     g.product = l;

@@ -21,23 +21,6 @@ struct BackwardArgs {
   QView gate, up, d, dt, ht;
 };
 
-struct Values8 {
-  float v[8];
-};
-// What 8 codes and their scale stand for.
-__device__ __forceinline__ Values8 f32_values(u32x2 codes, uint32_t code) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const float s = scale_operand(code);
-  Values8 r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x2 lo = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)codes[i], s, false));
-    const f32x2 hi = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)codes[i], s, true));
-    r.v[4 * i] = lo[0], r.v[4 * i + 1] = lo[1], r.v[4 * i + 2] = hi[0], r.v[4 * i + 3] = hi[1];
-  }
-  return r;
-}
-
 __device__ __forceinline__ uint32_t scale_at(const QView& q, uint32_t row, uint32_t block) {
   return q.scales[((int64_t)(block >> 2) * q.srows + row) * 4 + (block & 3)];
 }

@@ -22,12 +22,13 @@ struct GatedProduct {
   Act act;
   QView hq, gate, up;  // of launch_gated_codes; gate and up: data null: not wanted
 };
-// Into rows of c, m x n / 2, by the plan of the m x n product, which has no splits.
+// Into rows of c, m x n / 2, by product.plan, which has no splits.
 hipError_t launch_gated_rows(const GatedProduct& g, hipStream_t st);
 // Into 8 bits: tiles of 256 or 128 rows by 128 columns, of which the last `halved` ones of 256 rows are cut into two each.
-//   rows 0: as a product of fp32 sums and their join.
+//   rows 0: as a product of fp32 sums, by `sums`, and their join.
 struct GatedCodesPlan {
   uint32_t rows, halved;
+  ProductPlan sums;
 };
 GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast);
 hipError_t launch_gated_codes(const GatedProduct& g, const GatedCodesPlan& plan, hipStream_t st);

@@ -46,7 +46,7 @@ hipError_t launch_product(const ProductLaunch& l, hipStream_t st) {
   ProductArgs a;
   fill_args(a, l, l.n);
   const int size = l.c_bf16 ? 2 : 4;
-  const ProductPlan plan = plan_product(l.m, l.n, l.kb, l.fast);
+  const ProductPlan plan = l.plan ? *l.plan : plan_product(l.m, l.n, l.kb, l.fast);
   if (l.x || plan.kind == ProductPlan::kDirect || l.c_stride * size >= kMaxRowBytes) {
     launch_direct_kind<kSums>(a, l.x_bf16, plan.rows16, st);
   } else {

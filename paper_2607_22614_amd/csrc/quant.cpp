@@ -30,6 +30,9 @@ int quantize_checked(const void* src, int32_t type, int64_t rows, int64_t cols, 
   return hip_result(launch_quantize(l, st), what);
 }
 
+namespace {
+
+// Bytes of the splits' sums, whichever sums the caller asks for.
 uint64_t product_space(int64_t m, int64_t n, int64_t k) {
   uint64_t bytes = 0;
   for (bool fast : {false, true}) {
@@ -39,6 +42,10 @@ uint64_t product_space(int64_t m, int64_t n, int64_t k) {
   return bytes;
 }
 
+// Where the quantized rows of a linear layer lie in its workspace.
+struct LinearSpace {
+  uint64_t data, scales, product, total;
+};
 LinearSpace linear_space(int64_t m, int64_t n, int64_t k) {
   LinearSpace s{0, 0, 0, 0};
   if (m > kFusedRows) {
@@ -49,6 +56,8 @@ LinearSpace linear_space(int64_t m, int64_t n, int64_t k) {
   }
   return s;
 }
+
+}  // namespace
 
 // Times in us, measured on random codes.  A step of a 256 x 256 tile takes 1.34 (exact sums 2.7), of one 128 x 128 tile
 // alone on its CU 0.63 (0.78; 0.5 with four blocks staged) and of two of them together 0.96 (1.72); what a tile costs beside

@@ -72,12 +72,5 @@ inline int check_workspace(const void* p, uint64_t have, uint64_t need, const ch
 // Quantizes src into q and/or qt, whose shapes and pointers have been checked.
 int quantize_checked(const void* src, int32_t type, int64_t rows, int64_t cols, int64_t row_stride, const dr_qmatrix* q, const dr_qmatrix* qt,
                      hipStream_t st, const char* what);
-// Bytes of the splits' sums of an m x n product over k columns, whichever sums the caller asks for.
-uint64_t product_space(int64_t m, int64_t n, int64_t k);
-// Where the quantized rows of a linear layer lie in its workspace, and the splits' sums behind them.
-struct LinearSpace {
-  uint64_t data, scales, product, total;
-};
-LinearSpace linear_space(int64_t m, int64_t n, int64_t k);
 
 }  // namespace dr

@@ -196,6 +196,37 @@ __device__ __forceinline__ Raw8<true> bf16_values(u32x2 codes, uint32_t code) {
   return v;
 }
 
+// What codes and their scale stand for, in fp32.
+struct Values8 {
+  float v[8];
+};
+__device__ __forceinline__ void f32_values4(uint32_t codes, float scale, float* to) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 lo = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)codes, scale, false));
+  const f32x2 hi = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)codes, scale, true));
+  to[0] = lo[0], to[1] = lo[1], to[2] = hi[0], to[3] = hi[1];
+}
+__device__ __forceinline__ Values8 f32_values(u32x2 codes, uint32_t code) {
+  Values8 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) f32_values4(codes[i], scale_operand(code), r.v + 4 * i);
+  return r;
+}
+
+// Sum over the wave, in every lane: within rows of 16 lanes by DPP moves, then across the rows.
+template <int ctrl>
+__device__ __forceinline__ float dpp_sum(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = dpp_sum<0xb1>(v);   // quad_perm [1,0,3,2]
+  v = dpp_sum<0x4e>(v);   // quad_perm [2,3,0,1]
+  v = dpp_sum<0x141>(v);  // row_half_mirror
+  v = dpp_sum<0x140>(v);  // row_mirror
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
 // fp32 -> bf16, ties to even (the hardware convert).
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});

@@ -43,6 +43,16 @@ inline bool whole_pieces(const void* src, int64_t stride, int64_t cols, int64_t 
 // Lanes of a workgroup that takes a tile of 128 x 128; a launch of rows alone has fewer of them in all.
 constexpr int kTileLanes = 512;
 
+// How a product of 8-bit operands is cut: tiles of one of two sizes, and each tile's blocks over `splits` workgroups
+// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows, `rows16` times 16 of them
+// per workgroup.  The last `quartered` tiles of 256 x 256 are cut into tiles of 128 x 128 each.
+struct ProductPlan {
+  enum Kind { kDirect, kTile128, kTile256 } kind;
+  uint32_t splits;
+  uint32_t quartered;
+  uint32_t rows16;  // of kDirect: 1 to 4
+  double us;        // what it should take; 0 up to 32 rows
+};
 // c (m x n) = a (m x k) * b^T (n x k), kb = ceil(k / 128) column blocks.
 struct ProductLaunch {
   QView a, b;
@@ -55,21 +65,12 @@ struct ProductLaunch {
   bool c_bf16, accumulate, fast;
   bool sums;         // c is fp32 rows of part_stride(n) in the workspace: what each of the plan's splits sums goes there, m rows a split
   void* workspace;
+  const ProductPlan* plan;  // plan_product(m, n, kb, fast) where the caller has it
 };
 hipError_t launch_product(const ProductLaunch& l, hipStream_t st);
 // Rows that launch_product quantizes itself.
 constexpr uint32_t kFusedRows = 16;
 
-// How a product of 8-bit operands is cut: tiles of one of two sizes, and each tile's blocks over `splits` workgroups
-// whose fp32 sums lie in the workspace until a second kernel joins them; or the kernel for few rows, `rows16` times 16 of them
-// per workgroup.  The last `quartered` tiles of 256 x 256 are cut into tiles of 128 x 128 each.
-struct ProductPlan {
-  enum Kind { kDirect, kTile128, kTile256 } kind;
-  uint32_t splits;
-  uint32_t quartered;
-  uint32_t rows16;  // of kDirect: 1 to 4
-  double us;        // what it should take; 0 up to 32 rows
-};
 // Tiles of 16 columns per workgroup of the kernel for few rows, and its waves, by the columns of c.
 inline uint32_t direct_columns16(int64_t n) { return n <= 4096 ? 1 : n <= 9216 ? 2 : 4; }
 constexpr uint32_t direct_waves(uint32_t columns16) { return columns16 == 4 ? 4 : 8; }

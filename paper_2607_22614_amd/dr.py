@@ -615,7 +615,7 @@ class QMatrix:
     """An 8-bit matrix over two device tensors of one-byte elements, which it keeps: data [rows, at least
     cols rounded up to 128] with dense rows, and scales (dense, [ceil(ceil(cols/128)/4), block rows, 4])."""
 
-    __slots__ = ("data", "scales", "rows", "cols", "block_rows", "c", "ref")
+    __slots__ = ("data", "scales", "rows", "cols", "block_rows", "c", "ref", "device")
 
     def __init__(self, data, scales, rows: int, cols: int, block_rows: int = 1):
         need = dr_qmatrix_sizes(rows, cols, block_rows)
@@ -631,6 +631,7 @@ class QMatrix:
         self.data, self.scales, self.rows, self.cols, self.block_rows = data, scales, int(rows), int(cols), int(block_rows)
         self.c = dr_qmatrix(data.data_ptr(), scales.data_ptr(), self.rows, self.cols, stride, self.block_rows, 0)
         self.ref = ctypes.byref(self.c)
+        self.device = data.get_device()
 
     @classmethod
     def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "QMatrix":
@@ -695,13 +696,39 @@ def dr_qlinear_workspace(m: int, w: QMatrix) -> int:
 
 
 # ------------------------------------------------------------------ the gated feed-forward block
-def _on_current(where: str, *tensors) -> None:
-    """The calls run on the current device: a tensor of another one is refused (None and the like are skipped)."""
+_device = None  # () -> the current device's index
+
+
+def _find_device():
     import torch
-    current = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != current:
-            raise ValueError(f"{where}: a tensor on {t.device}, the current device is {current}")
+    torch.cuda.current_device()  # initialises torch's side of the GPU
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _forget_device():
+    global _device
+    _device = None
+
+
+os.register_at_fork(after_in_child=_forget_device)
+
+
+def _on_current(where: str, *devices: int) -> None:
+    """The calls run on the current device: what lies on another one is refused."""
+    global _device
+    if _device is None:
+        _device = _find_device()
+    current = _device()
+    for d in devices:
+        if d != current:
+            raise ValueError(f"{where}: an argument on device {d}, the current device is {current}")
+
+
+def _space(ws, where: str):
+    """(address, bytes) of a workspace tensor on the current device, or of None."""
+    if ws is not None:
+        _on_current(where, ws.get_device())
+    return _workspace(ws, where)
 
 
 def dr_qgated(x, w: QMatrix, out, act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
@@ -711,9 +738,9 @@ def dr_qgated(x, w: QMatrix, out, act: int = DR_ACT_SILU, fast: bool = False, wo
     oaddr, okind, orows, ocols, ostep = _dense_rows(out, "dr_qgated out")
     if cols != w.cols or orows != rows or 2 * ocols != w.rows:
         raise ValueError(f"dr_qgated: x {rows} x {cols}, w {w.rows} x {w.cols}, out {orows} x {ocols}")
-    _on_current("dr_qgated", x, w.data, out, workspace)
+    _on_current("dr_qgated", x.get_device(), w.device, out.get_device())
     _check(_lib.dr_qgated(addr, kind, rows, step, w.ref, act, oaddr, okind, ostep, DR_FAST_SUMS if fast else 0,
-                          *_workspace(workspace, "dr_qgated workspace"), _stream(stream)), "dr_qgated")
+                          *_space(workspace, "dr_qgated workspace"), _stream(stream)), "dr_qgated")
 
 
 def dr_qgated_workspace(m: int, w: QMatrix) -> int:
@@ -725,9 +752,10 @@ def dr_qgated_save(x: QMatrix, w: QMatrix, h: QMatrix, gate: QMatrix | None = No
                    act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
     """h = act(x w_gate^T) * (x w_up^T) in 8 bits, and the halves of x w^T as the checkpoint for dr_gated_backward;
     fast: DR_FAST_SUMS."""
-    _on_current("dr_qgated_save", x.data, w.data, h.data, gate and gate.data, up and up.data, workspace)
+    _on_current("dr_qgated_save", x.device, w.device, h.device, gate.device if gate else h.device,
+                up.device if up else h.device)
     _check(_lib.dr_qgated_save(x.ref, w.ref, act, h.ref, gate and gate.ref, up and up.ref, DR_FAST_SUMS if fast else 0,
-                               *_workspace(workspace, "dr_qgated_save workspace"), _stream(stream)), "dr_qgated_save")
+                               *_space(workspace, "dr_qgated_save workspace"), _stream(stream)), "dr_qgated_save")
 
 
 def dr_qgated_save_workspace(m: int, w: QMatrix) -> int:
@@ -742,14 +770,14 @@ def dr_gated_backward(dh, gate: QMatrix, up: QMatrix, d: QMatrix | None = None, 
     addr, kind, rows, cols, step = _dense_rows(dh, "dr_gated_backward dh")
     if rows != gate.rows or cols != gate.cols:
         raise ValueError(f"dr_gated_backward: dh {rows} x {cols}, gate {gate.rows} x {gate.cols}")
-    _on_current("dr_gated_backward", dh, gate.data, up.data, d and d.data, dt and dt.data, ht and ht.data)
+    _on_current("dr_gated_backward", dh.get_device(), gate.device, up.device, *[q.device for q in (d, dt, ht) if q])
     _check(_lib.dr_gated_backward(addr, kind, step, gate.ref, up.ref, act, d and d.ref, dt and dt.ref, ht and ht.ref,
                                   _stream(stream)), "dr_gated_backward")
 
 
 def dr_qtranspose(src: QMatrix, qt: QMatrix, stream=None) -> None:
     """qt = the transpose of src, quantized anew in blocks of 1 x 128."""
-    _on_current("dr_qtranspose", src.data, qt.data)
+    _on_current("dr_qtranspose", src.device, qt.device)
     _check(_lib.dr_qtranspose(src.ref, qt.ref, _stream(stream)), "dr_qtranspose")
 
 

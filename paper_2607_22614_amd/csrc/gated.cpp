@@ -41,16 +41,20 @@ int check_halves(const dr_qmatrix* w, const char* what) {
 struct GatedSpace {
   uint64_t data, scales, sums;
 };
-GatedSpace gated_space(int64_t m, int64_t k) {
-  if (m <= kFusedRows) return {0, 0, 0};
+GatedSpace gated_space(int64_t m, int64_t k, bool fused) {
+  if (fused) return {0, 0, 0};
   const uint64_t scales = (uint64_t)m * padded(k);
   return {0, scales, (scales + (uint64_t)ceil_div(padded(k) / kBlock, 4) * m * 4 + 15) / 16 * 16};
 }
 uint64_t sums_space(int64_t m, int64_t f, uint32_t splits) {
   return splits * (uint64_t)m * part_stride(2 * f) * sizeof(float) + 16;  // the join reads whole 16 bytes
 }
-uint64_t rows_need(int64_t m, int64_t f, int64_t k, const ProductPlan& plan) {
-  return gated_space(m, k).sums + (plan.splits > 1 ? sums_space(m, f, plan.splits) : 0);
+uint64_t rows_need(int64_t m, int64_t f, int64_t k, const GatedRowsPlan& plan) {
+  return gated_space(m, k, plan.fused).sums + (plan.product.splits > 1 ? sums_space(m, f, plan.product.splits) : 0);
+}
+// Whatever x's type.
+uint64_t rows_most(int64_t m, int64_t f, int64_t k, bool fast) {
+  return rows_need(m, f, k, {m <= kFusedRows, plan_product(m, 2 * f, ceil_div(k, kBlock), fast)});
 }
 uint64_t save_need(int64_t m, int64_t f, const GatedCodesPlan& plan) { return plan.rows ? 0 : sums_space(m, f, plan.sums.splits); }
 
@@ -100,6 +104,20 @@ int product_and_join(ProductLaunch l, GatedJoin& j, uint8_t* sums, Act act, hipS
 
 }  // namespace
 
+// Beyond kFusedRows rows of x a launch of its own quantizes them, which takes 2 us between others and, with the host's calls for
+// two launches, 8.5 at least; in the product's kernel, where every workgroup quantizes what it reads, x costs 1.5 and a tenth
+// of the product, in fp32 1.8 and seven tenths.  In us, apart / in the product's kernel, launched by the host: 333 x 344 x 256
+// fp32 8.8 / 6.9, bf16 8.4 / 6.2; 100 x 1000 x 1000 8.9 / 6.3; 32 x 4864 x 896 8.6 / 7.1; 61 x 4864 x 896 10.0 / 10.5; 20 x 3584 x
+// 4096 11.8 / 12.7; 40 x 2000 x 2000 8.6 / 9.4.  With 64 instead of 32 rows a workgroup the latter lose 10 to 50 %.
+GatedRowsPlan plan_gated_rows(int64_t m, int64_t f, int64_t k, bool x_bf16, bool fast) {
+  const int64_t kb = ceil_div(k, kBlock);
+  const GatedRowsPlan plan{m <= kFusedRows, plan_product(m, 2 * f, kb, fast)};
+  if (plan.fused || k < 8) return plan;
+  const double direct = direct_us(m, 2 * f, kb, 2), inside = x_bf16 ? 1.1 * direct + 1.5 : 1.7 * direct + 1.8;
+  const double apart = std::max((m <= 32 ? direct : plan.product.us) + 2, 8.5);
+  return inside < apart ? GatedRowsPlan{true, {ProductPlan::kDirect, 1, 0, 2, inside}} : plan;
+}
+
 GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast) {
   const ProductPlan sums = plan_product(m, 2 * f, kb, fast);
   if (m <= 32 || !kb) return {0, 0, sums};
@@ -125,7 +143,7 @@ using namespace dr;
 extern "C" int dr_qgated_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
   clear_error();
   return workspace_of(m, f, k, bytes, "dr_qgated_workspace",
-                      [=](bool fast) { return rows_need(m, f, k, plan_product(m, 2 * f, ceil_div(k, kBlock), fast)); });
+                      [=](bool fast) { return rows_most(m, f, k, fast); });
 }
 
 extern "C" int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes) {
@@ -148,13 +166,13 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
   if (int rc = check_sizes(m, f, k, what)) return rc;
   if (!m || !f) return DR_OK;
   ProductLaunch l = product_with(*w, m, (flags & DR_FAST_SUMS) != 0);
-  const ProductPlan plan = plan_product(m, 2 * f, l.kb, l.fast);
+  const GatedRowsPlan plan = plan_gated_rows(m, f, k, x_type == DR_TYPE_BF16, l.fast);
   if (int rc = check_workspace(workspace, workspace_bytes, rows_need(m, f, k, plan), what)) return rc;
-  l.plan = &plan;
+  l.plan = &plan.product;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const GatedSpace s = gated_space(m, k);
+  const GatedSpace s = gated_space(m, k, plan.fused);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (m <= kFusedRows) {
+  if (plan.fused) {
     l.x = x;
     l.x_stride = x_row_stride;
     l.x_bf16 = x_type == DR_TYPE_BF16;
@@ -167,7 +185,7 @@ extern "C" int dr_qgated(const void* x, int32_t x_type, int64_t m, int64_t x_row
   l.c = h;
   l.c_stride = h_row_stride;
   l.c_bf16 = h_type == DR_TYPE_BF16;
-  if (plan.splits == 1) {
+  if (plan.product.splits == 1) {
     GatedProduct g;
     std::memset(&g, 0, sizeof(g));
     g.product = l;

@@ -24,6 +24,12 @@ struct GatedProduct {
 };
 // Into rows of c, m x n / 2, by product.plan, which has no splits.
 hipError_t launch_gated_rows(const GatedProduct& g, hipStream_t st);
+//   fused: x is quantized in the product's kernel (whose plan's rows16 is 1 or 2).
+struct GatedRowsPlan {
+  bool fused;
+  ProductPlan product;
+};
+GatedRowsPlan plan_gated_rows(int64_t m, int64_t f, int64_t k, bool x_bf16, bool fast);
 // Into 8 bits: tiles of 256 or 128 rows by 128 columns, of which the last `halved` ones of 256 rows are cut into two each.
 //   rows 0: as a product of fp32 sums, by `sums`, and their join.
 struct GatedCodesPlan {

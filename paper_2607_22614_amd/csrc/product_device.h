@@ -285,18 +285,20 @@ void launch_few_rows(const ArgsOf<RESULTS>& a, hipStream_t st) {
   else launch_direct<4, TT, direct_waves(4), X, RESULTS>(a, st);
 }
 
-// x quantized in the kernel, or a's codes and `rows16` times 16 rows per workgroup.
+// x quantized in the kernel, or a's codes; `rows16` times 16 rows per workgroup (of x: 1, for pairs of rows of b 1 or 2).
+template <int X, int RESULTS>
+void launch_direct_x(const ArgsOf<RESULTS>& a, uint32_t rows16, hipStream_t st) {
+  if (a.a.cols < 8) return launch_direct<1, 1, 8, X | kShort, RESULTS>(a, st);
+  if constexpr (RESULTS != kSums) {
+    if (rows16 == 2) return launch_few_rows<2, X, RESULTS>(a, st);
+  }
+  launch_few_rows<1, X, RESULTS>(a, st);
+}
 template <int RESULTS>
 void launch_direct_kind(const ArgsOf<RESULTS>& a, bool x_bf16, uint32_t rows16, hipStream_t st) {
   if (a.x) {
-    const bool shorter = a.a.cols < 8;
-    if (x_bf16) {
-      if (shorter) launch_direct<1, 1, 8, kBf16 | kShort, RESULTS>(a, st);
-      else launch_few_rows<1, kBf16, RESULTS>(a, st);
-    } else {
-      if (shorter) launch_direct<1, 1, 8, kF32 | kShort, RESULTS>(a, st);
-      else launch_few_rows<1, kF32, RESULTS>(a, st);
-    }
+    if (x_bf16) launch_direct_x<kBf16, RESULTS>(a, rows16, st);
+    else launch_direct_x<kF32, RESULTS>(a, rows16, st);
     return;
   }
   switch (rows16) {

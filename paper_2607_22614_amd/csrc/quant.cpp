@@ -67,18 +67,22 @@ LinearSpace linear_space(int64_t m, int64_t n, int64_t k) {
 // 4.5 TB/s.  Over 83 shapes from 48 x 2000 x 2000 to 3000 x 32064 x 4096 the choice takes at most 11 % more than the
 // best of eight ways with tiles and three with the kernel for few rows, in another session 19 % (200 x 4096 x 3584); that kernel
 // brings 48 x 2000 x 2000 from 10.0 to 6.7, 200 x 688 x 256 from 5.4 to 3.7.
+double direct_us(int64_t m, int64_t n, int64_t kb, uint32_t rows16) {
+  constexpr double direct_step[3][3] = {{1.45, 1.72, 2.45}, {1.88, 2.3, 2.9}, {1.35, 1.75, 2.1}}, direct_start[3] = {1.8, 3, 3};
+  const uint32_t columns16 = direct_columns16(n), waves = direct_waves(columns16), wide = columns16 / 2;
+  const double blocks = kb < waves ? (double)kb / waves : (double)ceil_div(kb, waves);
+  const double rounds = std::ceil((double)ceil_div(n, 16 * columns16) * (double)ceil_div(m, 16 * rows16) / 256);
+  return std::max(direct_start[wide] + rounds * blocks * direct_step[wide][rows16 - 2] + 0.5 * (rounds - 1), 2 + 128.0 * (double)kb * (double)n / 4.5e6);
+}
+
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast) {
   if (m <= 32 || !kb) return {ProductPlan::kDirect, 1, 0, m <= 16 ? 1u : 2u, 0};
   constexpr double kCus = 256;
   const double step256 = fast ? 1.34 : 2.7, step128 = fast ? 0.63 : 0.78, pair128 = fast ? 0.96 : 1.72;
   ProductPlan best{ProductPlan::kTile256, 1, 0, 2, 0};
   double least = HUGE_VAL;
-  constexpr double direct_step[3][3] = {{1.45, 1.72, 2.45}, {1.88, 2.3, 2.9}, {1.35, 1.75, 2.1}}, direct_start[3] = {1.8, 3, 3};
-  const uint32_t columns16 = direct_columns16(n), waves = direct_waves(columns16), wide = columns16 / 2;
-  const double blocks = kb < waves ? (double)kb / waves : (double)ceil_div(kb, waves);
   for (uint32_t rows16 = 2; rows16 <= 4; ++rows16) {
-    const double rounds = std::ceil((double)ceil_div(n, 16 * columns16) * (double)ceil_div(m, 16 * rows16) / kCus);
-    const double us = std::max(direct_start[wide] + rounds * blocks * direct_step[wide][rows16 - 2] + 0.5 * (rounds - 1), 2 + 128.0 * (double)kb * (double)n / 4.5e6);
+    const double us = direct_us(m, n, kb, rows16);
     if (us < least) least = us, best = {ProductPlan::kDirect, 1, 0, rows16, us};
   }
   for (const auto kind : {ProductPlan::kTile256, ProductPlan::kTile128}) {

@@ -85,5 +85,7 @@ constexpr int64_t kMaxRowBytes = 1ll << 24;
 inline int64_t part_stride(int64_t n) { return ceil_div(n, 4) * 4; }
 
 ProductPlan plan_product(int64_t m, int64_t n, int64_t kb, bool fast);
+// What the kernel for few rows should take, with rows16 times 16 rows a workgroup; rows16 from 2 to 4.
+double direct_us(int64_t m, int64_t n, int64_t kb, uint32_t rows16);
 
 }  // namespace dr

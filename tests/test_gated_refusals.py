@@ -42,10 +42,10 @@ def test_matrices(bad, text):
 
 
 def test_gated():
-    lib, w = dr._lib, _q(14, 200, 128)
-    need = dr._bytes(lib.dr_qgated_workspace, "", 100, 7, 200)
+    lib, w = dr._lib, _q(4000, 2000, 128)
+    need = dr._bytes(lib.dr_qgated_workspace, "", 300, 2000, 2000)
 
-    def call(x=P, x_type=0, m=100, x_stride=200, w=w, act=0, h=P, h_type=0, h_stride=7, flags=0, ws=P, have=need):
+    def call(x=P, x_type=0, m=300, x_stride=2000, w=w, act=0, h=P, h_type=0, h_stride=2000, flags=0, ws=P, have=need):
         return lib.dr_qgated(x, x_type, m, x_stride, w, act, h, h_type, h_stride, flags, ws, have, None)
 
     _refused(call(w=None), "w is null")
@@ -57,15 +57,15 @@ def test_gated():
     _refused(call(x=0), "x is null or misaligned")
     _refused(call(x=P + 2), "x is null or misaligned")
     _refused(call(x_type=2), "unknown type")
-    _refused(call(x_stride=199), "row stride")
+    _refused(call(x_stride=1999), "row stride")
     _refused(call(h=0), "h is null or misaligned")
     _refused(call(h=P + 1, h_type=1), "h is null or misaligned")
     _refused(call(h_type=5), "unknown type")
-    _refused(call(h_stride=6), "row stride")
+    _refused(call(h_stride=1999), "row stride")
     _refused(call(flags=1), "unknown flags")
     _refused(call(flags=4), "unknown flags")
     assert need > 0
-    _refused(call(have=need - 1), "workspace")
+    _refused(call(have=300 * 2048), "workspace")
     _refused(call(ws=None), "workspace")
     _refused(call(ws=P + 8), "workspace")
     big = _q((1 << 26) - 2, 128, 128)

@@ -266,7 +266,7 @@ extern "C" int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row
   if (ht) {
     if (int rc = check_rows_matrix(ht, f, m, what, "ht")) return rc;
   }
-  const int64_t tiles = backward_tiles_x(f) * ceil_div(m, kBlock);
+  const int64_t tiles = ceil_div(2 * f, kBlock) * ceil_div(m, kBlock);
   if (tiles > max_workgroups(kTileLanes)) return fail(DR_EINVAL, "%s: %lld x %lld is 2^23 or more tiles", what, (long long)m, (long long)f);
   if (!m || !f) return DR_OK;
   GatedBackward l;

@@ -63,7 +63,5 @@ struct GatedBackward {
   QView gate, up, d, dt, ht;
 };
 hipError_t launch_gated_backward(const GatedBackward& l, hipStream_t st);
-// Columns of tiles that launch_gated_backward takes.
-inline int64_t backward_tiles_x(int64_t f) { return f % kBlock ? ceil_div(2 * f, kBlock) : f / kBlock; }
 
 }  // namespace dr

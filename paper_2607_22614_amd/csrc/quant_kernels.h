@@ -40,6 +40,8 @@ hipError_t launch_turn(const QView& src, const QView& qt, hipStream_t st);
 inline bool whole_pieces(const void* src, int64_t stride, int64_t cols, int64_t size) {
   return reinterpret_cast<uintptr_t>(src) % 16 == 0 && stride * size % 16 == 0 && cols * size % 16 == 0;
 }
+// Bytes moved by a call from which on its sources are streamed past the caches (quantize.hip).
+constexpr int64_t kCached = 96ll << 20;
 // Lanes of a workgroup that takes a tile of 128 x 128; a launch of rows alone has fewer of them in all.
 constexpr int kTileLanes = 512;
 

@@ -28,7 +28,7 @@ struct QuantizeArgs {
 // 3001 that way).  Streamed loads leave the last cache (256 MiB) to what the call writes, and
 // do not profit from a source that lies there.  Between calls that go round among a few sets of buffers they win where all
 // of the sets together pass the cache: from 128 MiB moved by a call with 2 sets, about 90 with 3, 64 to 72 with 4.  A
-// call does not know the others; kCached is the line for somewhat less than 3.  In us, plain / streamed:
+// call does not know the others; kCached (quant_kernels.h) is the line for somewhat less than 3.  In us, plain / streamed:
 //                                  3 sets         from HBM       just written
 //   4096 x 4096 bf16, rows       10.6 / 11.3     12.6 / 11.0     12.5 / 12.7
 //   8192 x 4096 bf16, both ways  28.2 / 26.4     28.7 / 29.0     22.7 / 25.9
@@ -36,7 +36,6 @@ struct QuantizeArgs {
 //   8192 x 14336 bf16, rows                      66.9 / 64.7     57.5 / 61.7
 //   16384 x 4096 fp32, rows      63.1 / 60.2
 //   16384 x 4096 fp32, both ways 75.3 / 82.0, where it does not pay
-constexpr int64_t kCached = 96ll << 20;
 template <bool BF16, int ROWS>
 __device__ __forceinline__ void load_rows(const QuantizeArgs& a, uint32_t row0, uint32_t col, Raw8<BF16> (&v)[ROWS]) {
   auto each = [&](auto load) {

@@ -17,8 +17,9 @@ int check_act(int32_t act, const char* what) {
 }
 
 Act act_of(int32_t act) {
-  const double k1 = 2.0 * std::sqrt(2.0 / 3.14159265358979323846);
-  return act == DR_ACT_SILU ? Act{1.0f, 0.0f} : Act{(float)k1, (float)(0.044715 * k1)};
+  constexpr double kMinusLog2e = -1.44269504088896340736;
+  const double k1 = act == DR_ACT_SILU ? 1.0 : 2.0 * std::sqrt(2.0 / 3.14159265358979323846), k3 = act == DR_ACT_SILU ? 0.0 : 0.044715 * k1;
+  return Act{(float)k1, (float)k3, (float)(kMinusLog2e * k1), (float)(kMinusLog2e * k3)};
 }
 
 // An 8-bit matrix of rows x cols in blocks of 1 x 128, as activations and gradients are.

@@ -8,13 +8,11 @@
 
 namespace dr {
 
-constexpr float kMinusLog2e = -1.44269504088896340736f;
-
-// z of act, times -log2(e).  g is cut off at 128, where the logistic function is 0 or 1 in fp32 for either activation: an infinite
+// z of act, times -log2(e), which the constants hold.  g is cut off at 128, where the logistic function is 0 or 1 in fp32 for either activation: an infinite
 // g or g^2 would make 0 * inf in z.
 __device__ __forceinline__ float exponent(float g, const Act& act) {
   const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
-  return c * fmaf(c * c, act.k3, act.k1) * kMinusLog2e;
+  return c * fmaf(c * c, act.n3, act.n1);
 }
 
 // The exponent is rounded to fp32, so the logistic function is off by (6 + |z|) 2^-23 of itself at most, and it is 0 where e^-z
@@ -31,7 +29,7 @@ struct ActSlope {
 template <bool SILU>
 __device__ __forceinline__ ActSlope act_slope(float g, const Act& act) {
   if (SILU) {
-    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * kMinusLog2e)), a = g * s;
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * act.n1)), a = g * s;
     return ActSlope{a, fmaf(a, 1.0f - s, s)};
   }
   const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(exponent(g, act))), a = g * s, c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);

@@ -14,6 +14,7 @@ namespace dr {
 // with k1 = 2 sqrt(2 / pi), k3 = 0.044715 k1.
 struct Act {
   float k1, k3;
+  float n1, n3;  // times -log2(e): e^-z = 2^(g (n1 + n3 g^2))
 };
 
 // The product with the fused weights (b: gate's rows, then up's; n: all of them), with act(gate) * up in place of its sums.

@@ -484,8 +484,18 @@ __device__ __forceinline__ void store_codes(const GatedArgs& p, const f32x16 (&a
         v[2][x][i] = here(acc[2 * x + 1][y][i]);
         v[0][x][i] = gated(v[1][x][i], v[2][x][i], p.act);
 #pragma unroll
-        for (int o = 0; o < 3; ++o) most[o] = fmaxf(most[o], finite_magnitude(v[o][x][i]));
+        for (int o = 0; o < 3; ++o) most[o] = fmaxf(most[o], fabsf(v[o][x][i]));
       }
+    if (__any(__float_as_uint(fmaxf(fmaxf(most[0], most[1]), most[2])) >= kInfBits)) {
+#pragma unroll
+      for (int o = 0; o < 3; ++o) {
+        most[o] = 0;
+#pragma unroll
+        for (int x = 0; x < TN / 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most[o] = fmaxf(most[o], finite_magnitude(v[o][x][i]));
+      }
+    }
     const uint32_t place = kMaxima + y % 2 * 3 * 32 * 4 + r * 4;
 #pragma unroll
     for (int o = 0; o < 3; ++o) {

@@ -103,6 +103,22 @@ __device__ __forceinline__ void settle8(Raw8<BF16>& v, uint32_t s) {
   for (int i = 0; i < kWords; ++i) v.w[i / 4][i % 4] = w[i];
 }
 
+// The 8 elements s places further on (s < 8), zeros in front of them.
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> delayed8(const Raw8<BF16>& v, uint32_t s) {
+  constexpr int kWords = BF16 ? 4 : 8, kPer = 8 / kWords;  // elements in a word
+  Raw8<BF16> r = v;
+#pragma unroll
+  for (int d = kWords / 2; d; d /= 2)
+#pragma unroll
+    for (int i = kWords - 1; i >= 0; --i) r.w[i / 4][i % 4] = s & (d * kPer) ? (i >= d ? r.w[(i - d) / 4][(i - d) % 4] : 0u) : r.w[i / 4][i % 4];
+  if (BF16) {
+#pragma unroll
+    for (int i = kWords - 1; i >= 0; --i) r.w[i / 4][i % 4] = s & 1 ? r.w[i / 4][i % 4] << 16 | (i ? r.w[(i - 1) / 4][(i - 1) % 4] >> 16 : 0u) : r.w[i / 4][i % 4];
+  }
+  return r;
+}
+
 // fp32 bits of element i.
 template <bool BF16>
 __device__ __forceinline__ uint32_t bits_of(const Raw8<BF16>& v, int i) {

@@ -33,17 +33,17 @@ constexpr uint32_t kBandT = 4, kTurn = 32;
 struct TilePlace {
   uint32_t rt, ct, row0, col;
 };
-// The t-th tile, in bands of BAND tiles down.
+// The t-th of `tiles` tiles, in bands of BAND tiles down.
 template <uint32_t BAND>
-__device__ __forceinline__ TilePlace place_of(uint32_t t, uint32_t tiles_x) {
+__device__ __forceinline__ TilePlace place_of(uint32_t t, uint32_t tiles, uint32_t tiles_x) {
   const uint32_t tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const uint32_t tiles_y = gridDim.x / tiles_x, band = t / (BAND * tiles_x);
+  const uint32_t tiles_y = tiles / tiles_x, band = t / (BAND * tiles_x);
   const uint32_t high = min(BAND, tiles_y - band * BAND), i_band = t - band * BAND * tiles_x;
   const uint32_t rt = band * BAND + i_band % high, ct = i_band / high;
   return TilePlace{rt, ct, rt * 128 + ty * kTileRows, ct * 128 + tx * 8};
 }
 
-__device__ __forceinline__ TilePlace tile_place(uint32_t tiles_x) { return place_of<kBandT>(xcd_group<kTurn>(blockIdx.x, gridDim.x), tiles_x); }
+__device__ __forceinline__ TilePlace tile_place(uint32_t tiles_x) { return place_of<kBandT>(xcd_group<kTurn>(blockIdx.x, gridDim.x), gridDim.x, tiles_x); }
 
 // Codes and scales of a tile whose elements behind the matrix's last row and column are 0: into q as they are (ROWS) and
 // into qt, whose rows are q's columns (COLS).  SQUARE: one scale for the tile, else one per row (DPP) and one per column (over

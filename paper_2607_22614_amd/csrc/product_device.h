@@ -279,7 +279,8 @@ void launch_direct(ArgsOf<RESULTS> a, hipStream_t st) {
 // workgroup reads: 6912 x 5120 take 9.3 us for one row.  More blocks in flight per wave (2 to 6) lost 5 to 50 %.
 template <int TT, int X, int RESULTS>
 void launch_few_rows(const ArgsOf<RESULTS>& a, hipStream_t st) {
-  const uint32_t columns16 = direct_columns16(RESULTS == kSums ? a.n : 2 * (int64_t)a.n);
+  // pairs: two tiles as long as all of them run at once (16 rows of x, 4600 pairs of 8192 columns: 31.4 us with two, 24.9 with four)
+  const uint32_t columns16 = RESULTS == kSums ? direct_columns16(a.n) : a.n <= 2048 ? 1 : a.n <= 4096 ? 2 : 4;
   if (columns16 == 1) launch_direct<1, TT, direct_waves(1), X, RESULTS>(a, st);
   else if (columns16 == 2) launch_direct<2, TT, direct_waves(2), X, RESULTS>(a, st);
   else launch_direct<4, TT, direct_waves(4), X, RESULTS>(a, st);

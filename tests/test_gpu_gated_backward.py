@@ -85,6 +85,44 @@ def test_rows_at_any_element(f, offset, stride, dtype):
     check_rows(made["dt"], d.T, t_d.T, "dt")
 
 
+def test_rows_far_apart():
+    """Rows of dh 2^24 bytes and more apart, beyond the offsets of the kernel for whole tiles."""
+    dr = _dr()
+    say("backward, rows far apart")
+    m, f, stride = 3, 256, (1 << 23) + 8
+    gate, up, dh, gv, uv, dv = _inputs(dr, m, f, torch.bfloat16, 6)
+    buf = torch.zeros((m - 1) * stride + f, dtype=torch.bfloat16, device="cuda")
+    src = buf.as_strided((m, f), (stride, 1))
+    src.copy_(dh)
+    made = {"d": poisoned(dr, m, 2 * f), "dt": poisoned(dr, 2 * f, m), "ht": poisoned(dr, f, m)}
+    dr.dr_gated_backward(src, gate, up, **{n: v[0] for n, v in made.items()})
+    torch.cuda.synchronize()
+    d, h, t_d, t_h = _want(dv, gv, uv, SILU)
+    check_rows(made["d"], d, t_d, "d")
+    check_rows(made["dt"], d.T, t_d.T, "dt")
+    check_rows(made["ht"], h.T, t_h.T, "ht")
+
+
+# more tiles than the CUs hold three times, bands of sixteen tiles that are cut off, inputs that are streamed
+@pytest.mark.parametrize("m,f,dtype", [(2200, 1408, torch.bfloat16), (1700, 1500, torch.float32), (4100, 4224, torch.float32), (900, 2051, torch.bfloat16)])
+def test_large(m, f, dtype):
+    dr = _dr()
+    say("large backward", m, f, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    gate, up = dr.QMatrix.empty(m, f), dr.QMatrix.empty(m, f)
+    for q in (gate, up):
+        dr.dr_quantize(torch.randn((m, f), generator=gen, device="cuda") * torch.exp2(torch.randn((m, 1), generator=gen, device="cuda")), q)
+    gv, uv = (quant.values(q.data.cpu().numpy(), q.scales.cpu().numpy(), f, 1) for q in (gate, up))
+    dh = (torch.randn((m, f), generator=gen, device="cuda") * 1e-3).to(dtype)
+    made = {"d": poisoned(dr, m, 2 * f), "dt": poisoned(dr, 2 * f, m), "ht": poisoned(dr, f, m)}
+    dr.dr_gated_backward(dh, gate, up, **{n: v[0] for n, v in made.items()}, act=GELU)
+    torch.cuda.synchronize()
+    d, h, t_d, t_h = _want(dh.to(torch.float64).cpu().numpy(), gv, uv, GELU)
+    check_rows(made["d"], d, t_d, "d")
+    check_rows(made["dt"], d.T, t_d.T, "dt")
+    check_rows(made["ht"], h.T, t_h.T, "ht")
+
+
 @pytest.mark.parametrize("f", [128, 100])
 @pytest.mark.parametrize("kind", [SILU, GELU])
 def test_far_and_not_finite(f, kind):

@@ -579,9 +579,6 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
   const uint32_t items = items_of<CODES>(p);
   static_assert(!PAIRS || (kWaves == 4 && BN / WN % 64 == 0), "32 rows of a stage at a time, pairs within a wave");
   static_assert(!CODES || (WN == 2 && BN == 256), "a block of 128 columns a tile");
-  // of row `at` of b's part of a stage: the pair's place in the tile, and whether it is up's
-  auto pair_of = [](uint32_t at) { return at / 64 * 32 + at % 32; };
-  auto second_of = [](uint32_t at) { return at / 32 % 2; };
 
   // The copying side.  Rows [0, BM) of a stage are a's, the others b's.  What changes from tile to tile is the same for all
   // lanes (ProductSource).  Rows past the matrix are beyond the buffer; scale codes past it are some other row's (a
@@ -598,7 +595,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
   for (int i = 0; i < TM; ++i) acode[i] = 4 * ((wm + i * 32 + r) >> p.a.sh);
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
-    if constexpr (PAIRS) bcode[i] = pair_of(wn + i * 32 + r) + i % 2 * p.half;  // the row itself: up's first one may lie inside a square block
+    if constexpr (PAIRS) bcode[i] = pair_of(wn + i * 32 + r) + second_of(wn + i * 32) * p.half;  // the row itself: up's first one may lie inside a square block
     else bcode[i] = 4 * ((wn + i * 32 + r) >> p.b.sh);
   }
   const Buffer ascales = buffer_at(p.a.scales, (p.kb + 3) / 4 * p.a.srows * 4), bscales = buffer_at(p.b.scales, (p.kb + 3) / 4 * p.b.srows * 4);
@@ -615,7 +612,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
   }
   auto stage_codes = [&](uint8_t* to) {
     if (a_codes) copy_words_to_lds(ascales, code_at, source.acodes + source.block / 4 * p.a.srows * 4, to + kCodes + wave * 256);
-    else if constexpr (PAIRS) copy_words_to_lds(bscales, 4 * ((source.bfirst + code_at) >> p.b.sh), source.block / 4 * p.b.srows * 4, to + kCodes + wave * 256);
+    else if constexpr (PAIRS) copy_words_to_lds(bscales, pair_code_at(source.bfirst, code_at, p.b.sh), source.block / 4 * p.b.srows * 4, to + kCodes + wave * 256);
     else copy_words_to_lds(bscales, code_at, source.bcodes + source.block / 4 * p.b.srows * 4, to + kCodes + wave * 256);
   };
   auto advance = [&] { next_block(source, upcoming); };
@@ -629,7 +626,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
 #pragma unroll
     for (int t = 0; t < TM; ++t) s.a[t] = __builtin_amdgcn_raw_buffer_load_b8(ascales, (int)acode[t], (int)aat, 0);
 #pragma unroll
-    for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)(PAIRS ? 4 * ((source.bfirst + bcode[t]) >> p.b.sh) : bcode[t]), (int)bat, 0);
+    for (int t = 0; t < TN; ++t) s.b[t] = __builtin_amdgcn_raw_buffer_load_b8(bscales, (int)(PAIRS ? pair_code_at(source.bfirst, bcode[t], p.b.sh) : bcode[t]), (int)bat, 0);
     return s;
   };
 

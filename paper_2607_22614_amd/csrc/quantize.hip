@@ -100,7 +100,8 @@ __global__ __launch_bounds__(kTileLanes) void quantize_tile_kernel(QuantizeArgs 
 }
 
 // The transpose of an 8-bit matrix, quantized anew.  The values go through bf16, which holds them: 4 significant bits, and
-// what lies below 2^-133 counts as 0 as in the products.
+// what lies below 2^-133 counts as 0 as in the products.  8192 x 4096 in 12.5 us, 8192 x 14336 in 47.5 (5.0 TB/s), 7 vector
+// instructions an element; with those of quantize_tile, 11, 15.6 and 51.
 struct TurnArgs {
   QView src, qt;
   uint32_t tiles_x;

@@ -311,3 +311,87 @@ def test_large_not_finite():
         q.scales[:, 300] = q.scales[:, 299]
         want[300], t[300] = want[299], t[299]
         check_rows(one, want, np.where(np.isnan(t), 0.0, t), name)
+
+
+@pytest.mark.parametrize("f,k", [(3, 16384), (9, 16385), (20, 20000), (4200, 300)])
+@pytest.mark.parametrize("x_type", [torch.bfloat16, torch.float32])
+def test_one_row(f, k, x_type):
+    """One row at the ends of what its own kernel's LDS holds, and beyond."""
+    dr = _dr()
+    say("one row", f, k, x_type)
+    x, w, xv, wv = _inputs(dr, 1, f, k, x_type, k, extra=16)
+    (_, _, h), (_, _, tol) = _want(xv, wv, GELU)
+    out = torch.full((2, f), 7.0, device="cuda")
+    dr.dr_qgated(x.cuda(), w, out[:1], act=GELU, workspace=_space(dr, 1, w))
+    _close(out[:1], h, tol, False)
+    assert (out[1] == 7.0).all()
+
+
+@pytest.mark.parametrize("m", [1, 5, 40, 300])
+def test_weights_of_more_than_4_gib(m):
+    """up's rows, and gate's last ones, begin beyond 2^32 bytes."""
+    dr = _dr()
+    say("large weights", m)
+    f, k = 300001, 8192
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    codes = torch.randint(0, 120, (2 * f, k), generator=gen, device="cuda", dtype=torch.uint8) | torch.randint(0, 2, (2 * f, 1), generator=gen, device="cuda", dtype=torch.uint8) << 7
+    w = dr.QMatrix(codes, torch.full((k // 512, -(-2 * f // 128), 4), 114, dtype=torch.uint8, device="cuda"), 2 * f, k, 128)
+    x = torch.randn((m, k), generator=gen, device="cuda") * 0.01
+    at = torch.tensor([0, 1, 4097, 131071, 131072, 262143, 262144, 299999, f - 1], device="cuda")
+    wv = quant.E4M3[torch.cat([codes[at], codes[at + f]]).cpu().numpy()] * 2.0**(114 - 127)
+    xv = quant.values(*quant.quantize(x.to(torch.float64).cpu().numpy(), 1), k, 1)
+    (gate, up, h), (dg, du, tol) = _want(xv, wv, SILU)
+    out = torch.empty((m, f), device="cuda")
+    dr.dr_qgated(x, w, out, workspace=_space(dr, m, w))
+    _close(out[:, at], h, tol, False)
+    if m < 40:
+        return
+    xq, made = dr.QMatrix.empty(m, k), [dr.QMatrix.empty(m, f) for _ in range(3)]
+    dr.dr_quantize(x, xq)
+    dr.dr_qgated_save(xq, w, *made, workspace=_space(dr, m, w, save=True))
+    for q, want, t in zip(made, (h, gate, up), (tol, dg, du)):
+        per = q.scales.permute(1, 0, 2).reshape(m, -1)[:, at // 128].cpu().numpy()
+        got = quant.E4M3[q.data[:, at].cpu().numpy()] * 2.0**(per - 127.0)
+        assert (np.abs(got - want) <= np.maximum(2.0**-4 * np.abs(want), 2.0**(per - 137.0)) * (1 + 2.0**-20) + 2 * t).all()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with workspaces of their own, and what each gives alone."""
+    dr = _dr()
+    say("two streams")
+    jobs = []
+    for i, (m, f, k) in enumerate([(200, 700, 512), (1, 3000, 1024), (90, 1500, 2048), (600, 1300, 256)]):
+        x, w, _, _ = _inputs(dr, m, f, k, torch.bfloat16, i)
+        xq, h, out = dr.QMatrix.empty(m, k), dr.QMatrix.empty(m, f), torch.empty((m, f), dtype=torch.bfloat16, device="cuda")
+        xs = x.cuda()
+        dr.dr_quantize(xs, xq)
+        jobs.append((xs, xq, w, h, out, _space(dr, m, w), _space(dr, m, w, save=True)))
+
+    def run(job, stream=None):
+        xs, xq, w, h, out, ws, ws2 = job
+        dr.dr_qgated(xs, w, out, fast=True, workspace=ws, stream=stream)
+        dr.dr_qgated_save(xq, w, h, fast=True, workspace=ws2, stream=stream)
+
+    alone = []
+    for job in jobs:
+        run(job)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in (job[3].data, job[3].scales, job[4])])
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(5):
+        for job, stream in zip(jobs, streams):
+            run(job, stream)
+    torch.cuda.synchronize()
+    for job, want in zip(jobs, alone):
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((job[3].data, job[3].scales, job[4]), want))
+
+
+def test_another_device_is_refused(monkeypatch):
+    dr = _dr()
+    w, x, h = dr.QMatrix.empty(8, 128, 128), torch.empty((3, 128), device="cuda"), torch.empty((3, 4), device="cuda")
+    q, g, t = dr.QMatrix.empty(3, 128), dr.QMatrix.empty(3, 4), dr.QMatrix.empty(128, 3)
+    monkeypatch.setattr(dr, "_device", lambda: 1)
+    for call in (lambda: dr.dr_qgated(x, w, h), lambda: dr.dr_qgated_save(q, w, g), lambda: dr.dr_qtranspose(q, t),
+                 lambda: dr.dr_gated_backward(h, g, g, dr.QMatrix.empty(3, 8))):
+        with pytest.raises(ValueError, match="current device"):
+            call()

@@ -123,6 +123,45 @@ def test_large(m, f, dtype):
     check_rows(made["ht"], h.T, t_h.T, "ht")
 
 
+@pytest.mark.parametrize("m,f", [(33000, 131072), (131072, 33003)])
+def test_matrices_of_more_than_4_gib(m, f):
+    """Elements at the beginning, around 2^32 bytes and at the end of every matrix."""
+    dr = _dr()
+    say("large matrices", m, f)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def random(rows, cols):
+        q = dr.QMatrix.empty(rows, cols)
+        q.data.random_(0, 100, generator=gen)
+        q.data[:, cols:] = 0
+        q.scales.random_(118, 124, generator=gen)
+        return q
+
+    def values(q, rows, cols):
+        per = q.scales[cols[0] // 512:(cols[-1]) // 512 + 1, rows].permute(1, 0, 2).reshape(len(rows), -1).cpu().numpy()
+        per = per[:, (cols // 128) - cols[0] // 512 * 4]
+        scale = 2.0**(per - 127.0)
+        return quant.E4M3[q.data[rows][:, cols].cpu().numpy()] * scale, scale
+
+    gate, up = random(m, f), random(m, f)
+    dh = torch.randn((m, f), generator=gen, device="cuda", dtype=torch.bfloat16)
+    d, dt, ht, gt = dr.QMatrix.empty(m, 2 * f), dr.QMatrix.empty(2 * f, m), dr.QMatrix.empty(f, m), dr.QMatrix.empty(f, m)
+    dr.dr_gated_backward(dh, gate, up, d, dt, ht)
+    dr.dr_qtranspose(gate, gt)
+    torch.cuda.synchronize()
+    for r0 in (0, (1 << 32) // f // 128 * 128, (m - 1) // 128 * 128):
+        for c0 in (0, (1 << 32) // m // 128 * 128, (f - 1) // 128 * 128):
+            rows, cols = np.arange(r0, min(r0 + 128, m)), np.arange(c0, min(c0 + 128, f))
+            gv, uv = values(gate, rows, cols)[0], values(up, rows, cols)[0]
+            want, h, t_d, t_h = _want(dh[rows][:, cols].to(torch.float64).cpu().numpy(), gv, uv, SILU)
+            n = len(cols)
+            for q, i, j, w, t in ((d, rows, cols, want[:, :n], t_d[:, :n]), (d, rows, cols + f, want[:, n:], t_d[:, n:]),
+                                  (dt, cols, rows, want[:, :n].T, t_d[:, :n].T), (dt, cols + f, rows, want[:, n:].T, t_d[:, n:].T),
+                                  (ht, cols, rows, h.T, t_h.T), (gt, cols, rows, gv.T, 0.0)):
+                got, scale = values(q, i, j)
+                assert (np.abs(got - w) <= np.maximum(2.0**-4 * np.abs(w), 2.0**-10 * scale) * (1 + 2.0**-20) + 2 * t).all()
+
+
 @pytest.mark.parametrize("f", [128, 100])
 @pytest.mark.parametrize("kind", [SILU, GELU])
 def test_far_and_not_finite(f, kind):

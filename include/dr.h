@@ -643,7 +643,8 @@ enum { DR_ACT_SILU = 0, DR_ACT_GELU_TANH = 1 };
 
 /* h = act(x w_gate^T) * (x w_up^T): as dr_qlinear on w (x of M x K, quantized in
  * blocks of 1 x 128; sums and flags as there), with activation and product where
- * the sums stand.  h is M x F of h_type.
+ * the sums stand.  h is M x F of h_type.  (A single row's elements below 2^-133
+ * may count as what they are instead of zero.)
  *   x, h: device pointers, aligned to their types.
  *   workspace: device buffer (16-byte aligned) of at least the bytes that
  *   dr_qgated_workspace gives; may be NULL where that is 0.
@@ -673,7 +674,7 @@ int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes);
  *   ht = the transpose of act(gate) * up (F x M), again from the checkpoint,
  * each in 8 bits in blocks of 1 x 128, as dr_quantize gives it from the fp32
  * values.  Any of d, dt and ht may be NULL, but not all; F a multiple of 128 reads
- * its inputs once, another F twice.
+ * its inputs once (rows of dh less than 2^24 bytes apart), another F twice.
  * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, null or
  * misaligned pointers, 2^23 or more tiles of 128 x 128), DR_EHIP. */
 int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, const dr_qmatrix* gate,

@@ -193,6 +193,34 @@ def test_far_and_not_finite(f, kind):
     check_rows(made["ht"], h.T, t_h.T, "ht")
 
 
+@pytest.mark.parametrize("f", [128, 90])
+@pytest.mark.parametrize("kind", [SILU, GELU])
+def test_ends_of_fp32(f, kind):
+    """Gradients among fp32's subnormals, where a scale is no less than 2^-127 and a product is off by up to 2^-149 each time; and
+    such that pass its largest number, which become NaN."""
+    dr = _dr()
+    say("backward, ends of fp32", f, kind)
+    m = 24
+    rng = np.random.default_rng(4)
+    gate, gv = quantized(dr, rng.standard_normal((m, f)))
+    up, uv = quantized(dr, rng.choice([1.0, -0.5, 0.25, 2.0], (m, f)) * np.where(np.arange(m) < 16, 1.0, 2.0**60)[:, None])
+    dh = rng.choice([1.0, -1.5, 1.25, -1.75], (m, f)) * 2.0**np.concatenate([rng.integers(-148, -100, 16), rng.integers(80, 100, 8)])[:, None]
+    dh = dh.astype(np.float32)
+    made = {"d": poisoned(dr, m, 2 * f), "dt": poisoned(dr, 2 * f, m), "ht": poisoned(dr, f, m)}
+    dr.dr_gated_backward(torch.from_numpy(dh).cuda(), gate, up, **{n: v[0] for n, v in made.items()}, act=kind)
+    torch.cuda.synchronize()
+    d, h, t_d, t_h = _want(dh.astype(np.float64), gv, uv, kind)
+    step = 2.0**-148
+    dv = dh.astype(np.float64)
+    t_d = t_d + step * (2 + np.abs(np.concatenate([uv, dv], 1)))
+    # dh * up is formed first; where it passes fp32, dgate does
+    over = np.concatenate([np.abs(dv * uv) >= 2.0**128, np.zeros_like(dv, dtype=bool)], 1) | (np.abs(d) >= 2.0**128)
+    d = np.where(over, np.nan, d)
+    check_rows(made["d"], d, t_d, "d")
+    check_rows(made["dt"], d.T, t_d.T, "dt")
+    check_rows(made["ht"], h.T, t_h.T, "ht")
+
+
 def _check_turned(made, values):
     q, wide, scales = made
     codes, sc = quant.quantize(values.T, 1)

@@ -8,31 +8,30 @@
 
 namespace dr {
 
-// z of act, times -log2(e), which the constants hold.  g is cut off at 128, where the logistic function is 0 or 1 in fp32 for either activation: an infinite
-// g or g^2 would make 0 * inf in z.
-__device__ __forceinline__ float exponent(float g, const Act& act) {
-  const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
-  return c * fmaf(c * c, act.n3, act.n1);
+// 1 / (1 + e^-z).  g is cut off at 128, where that is 0 or 1 in fp32 for either activation: an infinite g or g^2 would make 0 * inf
+// in z.  Each rounding of the exponent costs up to |z| 2^-24 of e^-z; what its last product loses is known, and goes into the sum
+// with 1 by e^(z + d) = e^z (1 + d).  What stays is g^2, the inner sum and the constants: 1.02 |z| 2^-23 for gelu, 0.12 |z| 2^-23 for
+// silu, whose inner sum is a constant.  The exponential, the reciprocal and the sums between add 3 2^-23, so that the result is
+// off by (6 + |z|) 2^-23 of itself at most where e^-z is finite, and else 0.  With the product's loss left out it would be
+// 1.5 |z| 2^-23 for gelu; with that of g^2 taken in too, 0.6 |z| 2^-23, 8192 rows of 3456 x 5120 take 4 us more.
+template <bool SILU>
+__device__ __forceinline__ float logistic(float g, const Act& act) {
+  const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f), n = SILU ? act.n1 : fmaf(c * c, act.n3, act.n1);
+  const float t = c * n, lost = fmaf(c, n, -t);  // of -z log2(e), which the constants hold
+  return __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), fmaf(lost, 0.693147181f, 1.0f), 1.0f));
 }
 
-// The exponent is rounded to fp32, so the logistic function is off by (6 + |z|) 2^-23 of itself at most, and it is 0 where e^-z
-// is infinite.
-__device__ __forceinline__ float gated(float gate, float up, const Act& act) {
-  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(exponent(gate, act))) * up;
-}
+__device__ __forceinline__ float gated(float gate, float up, const Act& act) { return gate * logistic<false>(gate, act) * up; }
 
-// act, and act' = s + g s (1 - s) z'.  1 - s is off by 2^-23 at most, and so the slope by |z| 2^-21.  SILU: k1 = 1, k3 = 0, at half the
-// instructions.
+// act, and act' = s + g s (1 - s) z'.  1 - s is off by 2^-23 at most, and so the slope by |z| 2^-21.
 struct ActSlope {
   float act, slope;
 };
 template <bool SILU>
 __device__ __forceinline__ ActSlope act_slope(float g, const Act& act) {
-  if (SILU) {
-    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * act.n1)), a = g * s;
-    return ActSlope{a, fmaf(a, 1.0f - s, s)};
-  }
-  const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(exponent(g, act))), a = g * s, c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
+  const float s = logistic<SILU>(g, act), a = g * s;
+  if (SILU) return ActSlope{a, fmaf(a, 1.0f - s, s)};
+  const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
   return ActSlope{a, fmaf(a * fmaf(c * c, 3.0f * act.k3, act.k1), 1.0f - s, s)};
 }
 

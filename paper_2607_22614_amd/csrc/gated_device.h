@@ -23,7 +23,8 @@ __device__ __forceinline__ float logistic(float g, const Act& act) {
 
 __device__ __forceinline__ float gated(float gate, float up, const Act& act) { return gate * logistic<false>(gate, act) * up; }
 
-// act, and act' = s + g s (1 - s) z'.  1 - s is off by 2^-23 at most, and so the slope by |z| 2^-21.
+// act, and act' = s + g s (1 - s) z'.  1 - s is off by 2^-23 at most, and so the slope by |z| 2^-21.  1 - s comes first: it is 0 for
+// gates whose product with z' passes fp32.
 struct ActSlope {
   float act, slope;
 };
@@ -32,7 +33,7 @@ __device__ __forceinline__ ActSlope act_slope(float g, const Act& act) {
   const float s = logistic<SILU>(g, act), a = g * s;
   if (SILU) return ActSlope{a, fmaf(a, 1.0f - s, s)};
   const float c = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
-  return ActSlope{a, fmaf(a * fmaf(c * c, 3.0f * act.k3, act.k1), 1.0f - s, s)};
+  return ActSlope{a, fmaf(a * (1.0f - s), fmaf(c * c, 3.0f * act.k3, act.k1), s)};
 }
 
 __device__ __forceinline__ float element(const Raw8<false>& v, int i) { return __uint_as_float(bits_of<false>(v, i)); }

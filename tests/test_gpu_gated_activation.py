@@ -13,6 +13,7 @@ import pytest
 import torch
 
 from oracle import gated, quant
+from tests.gated_helpers import check_rows, poisoned, quantized
 from tests.gpu_helpers import say
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +82,27 @@ def test_negative_gates(m, f, k, kind, far, fast):
     bad = ~(np.abs(got - want) <= allowed * np.abs(want) + 2.0**-149) & ~(lost & (got == 0))
     off = np.abs(got / np.where(want == 0, 1, want) - 1) * 2.0**23
     assert not bad.any(), (int(bad.sum()), gate[bad][:4], z[bad][:4], off[bad][:4], got[bad][:4])
+
+
+@pytest.mark.parametrize("m,f", [(70, 5), (70, 100), (70, 120), (70, 128), (300, 384)])
+@pytest.mark.parametrize("kind", [SILU, GELU])
+def test_slopes_of_far_gates(m, f, kind):
+    """Gates up to fp32's ends have slopes of 1 and 0, and gradients that fp32 holds are not NaN."""
+    dr = _dr()
+    say("slopes of far gates", m, f, kind)
+    rng = np.random.default_rng(f)
+    gate, gv = quantized(dr, rng.choice([1.0, -1.0, 1.5, -1.75], (m, f)) * 2.0**rng.choice([60, 100, 113, 114, 116, 120, 126], (m, 1)))
+    up, uv = quantized(dr, rng.choice([1.0, -1.0, 0.75, 0.0], (m, f)))
+    dh = rng.choice([1.0, -0.5, 0.625, 0.0], (m, f)).astype(np.float32)
+    made = {"d": poisoned(dr, m, 2 * f), "dt": poisoned(dr, 2 * f, m), "ht": poisoned(dr, f, m)}
+    dr.dr_gated_backward(torch.from_numpy(dh).cuda(), gate, up, **{n: v[0] for n, v in made.items()}, act=kind)
+    torch.cuda.synchronize()
+    # slopes and logistic functions are whole here, so that nothing but dh, up and gate is multiplied: 3 roundings at most, and
+    # what is 2^-100 of the factors and below may count as 0
+    a, _, _ = gated.act(gv, kind)
+    dv = dh.astype(np.float64)
+    d, h = np.concatenate(gated.backward(dv, gv, uv, kind), 1), a * uv
+    tol = 3 * 2.0**-24
+    check_rows(made["d"], d, tol * np.abs(d) + 2.0**-100, "d")
+    check_rows(made["dt"], d.T, (tol * np.abs(d) + 2.0**-100).T, "dt")
+    check_rows(made["ht"], h.T, (tol * np.abs(h) + 2.0**-100).T, "ht")

@@ -570,6 +570,49 @@ def dr_break_even_steps(switch_cost_s: float, step_before_s: float, step_after_s
 
 
 # ------------------------------------------------------------------ 8-bit matrices
+def _find_device() -> None:
+    global _device, _raw_stream
+    import torch
+    torch.cuda.current_device()  # initialises torch's side of the GPU
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if _raw_stream is None:
+        _raw_stream = lambda d: torch.cuda.current_stream(d).cuda_stream  # noqa: E731
+
+
+def _first_device() -> int:
+    _find_device()
+    return _device()
+
+
+def _first_raw_stream(device: int) -> int:
+    _find_device()
+    return _raw_stream(device)
+
+
+def _forget_device():
+    global _device, _raw_stream
+    _device, _raw_stream = _first_device, _first_raw_stream
+
+
+_forget_device()  # _device(): the current device's index; _raw_stream(device): the handle of its current stream
+os.register_at_fork(after_in_child=_forget_device)
+
+
+def _elsewhere(where: str, *devices: int) -> None:
+    raise ValueError(f"{where}: arguments on devices {list(devices)}, the current device is {_device()}")
+
+
+def _stream_on(device: int, stream, where: str) -> int:
+    """The stream's handle, for a call with arguments on `device`: the calls run on the current one."""
+    current = _device()
+    if device != current:
+        _elsewhere(where, device)
+    if stream is None:
+        return _raw_stream(current)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
 _TYPES: dict = {}  # torch dtype -> DR_TYPE_*, filled at the first tensor
 
 
@@ -625,13 +668,15 @@ class QMatrix:
             raise ValueError(f"QMatrix: data is not [{rows}, at least {need['stride']}] with dense rows")
         if not scales.is_contiguous() or scales.numel() < need["scale_bytes"]:
             raise ValueError(f"QMatrix: scales are not {need['scale_bytes']} dense bytes")
+        self.device = data.get_device()
+        if scales.get_device() != self.device:
+            raise ValueError(f"QMatrix: data on device {self.device}, scales on {scales.get_device()}")
         stride = data.stride(0) if rows > 1 and cols else need["stride"]
         if stride < need["stride"]:
             raise ValueError("QMatrix: rows overlap")
         self.data, self.scales, self.rows, self.cols, self.block_rows = data, scales, int(rows), int(cols), int(block_rows)
         self.c = dr_qmatrix(data.data_ptr(), scales.data_ptr(), self.rows, self.cols, stride, self.block_rows, 0)
         self.ref = ctypes.byref(self.c)
-        self.device = data.get_device()
 
     @classmethod
     def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "QMatrix":
@@ -645,16 +690,21 @@ class QMatrix:
 def dr_quantize(src, q: QMatrix | None = None, qt: QMatrix | None = None, stream=None) -> None:
     """src (2-d float32 or bfloat16) to 8 bits: as it is into q, transposed into qt."""
     addr, kind, rows, cols, step = _dense_rows(src, "dr_quantize src")
+    device = src.get_device()
+    if q and q.device != device or qt and qt.device != device:
+        _elsewhere("dr_quantize", device, *[m.device for m in (q, qt) if m])
     _check(_lib.dr_quantize(addr, kind, rows, cols, step, q.ref if q else None, qt.ref if qt else None,
-                            _stream(stream)), "dr_quantize")
+                            _stream_on(device, stream, "dr_quantize")), "dr_quantize")
 
 
-def _workspace(ws, where: str):
-    """(address, bytes) of a workspace tensor or None."""
+def _workspace(ws, device: int, where: str):
+    """(address, bytes) of a workspace tensor on `device`, or of None."""
     if ws is None:
         return 0, 0
     if not ws.is_cuda or not ws.is_contiguous():
         raise ValueError(f"{where}: expected a dense device tensor")
+    if ws.get_device() != device:
+        _elsewhere(where, ws.get_device())
     return ws.data_ptr(), ws.nbytes
 
 
@@ -664,9 +714,13 @@ def dr_qmatmul(a: QMatrix, b: QMatrix, out, accumulate: bool = False, fast: bool
     addr, kind, rows, cols, step = _dense_rows(out, "dr_qmatmul out")
     if rows != a.rows or cols != b.rows:
         raise ValueError(f"dr_qmatmul out: {rows} x {cols}, the product is {a.rows} x {b.rows}")
+    device = a.device
+    if not device == b.device == out.get_device():
+        _elsewhere("dr_qmatmul", device, b.device, out.get_device())
     _check(_lib.dr_qmatmul(a.ref, b.ref, addr, kind, step,
                            (DR_ACCUMULATE if accumulate else 0) | (DR_FAST_SUMS if fast else 0),
-                           *_workspace(workspace, "dr_qmatmul workspace"), _stream(stream)), "dr_qmatmul")
+                           *_workspace(workspace, device, "dr_qmatmul workspace"),
+                           _stream_on(device, stream, "dr_qmatmul")), "dr_qmatmul")
 
 
 def _bytes(call, where: str, *args) -> int:
@@ -686,8 +740,12 @@ def dr_qlinear(x, w: QMatrix, out, fast: bool = False, workspace=None, stream=No
     oaddr, okind, orows, ocols, ostep = _dense_rows(out, "dr_qlinear out")
     if cols != w.cols or orows != rows or ocols != w.rows:
         raise ValueError(f"dr_qlinear: x {rows} x {cols}, w {w.rows} x {w.cols}, out {orows} x {ocols}")
+    device = w.device
+    if not device == x.get_device() == out.get_device():
+        _elsewhere("dr_qlinear", x.get_device(), device, out.get_device())
     _check(_lib.dr_qlinear(addr, kind, rows, step, w.ref, oaddr, okind, ostep, DR_FAST_SUMS if fast else 0,
-                           *_workspace(workspace, "dr_qlinear workspace"), _stream(stream)), "dr_qlinear")
+                           *_workspace(workspace, device, "dr_qlinear workspace"),
+                           _stream_on(device, stream, "dr_qlinear")), "dr_qlinear")
 
 
 def dr_qlinear_workspace(m: int, w: QMatrix) -> int:
@@ -696,41 +754,6 @@ def dr_qlinear_workspace(m: int, w: QMatrix) -> int:
 
 
 # ------------------------------------------------------------------ the gated feed-forward block
-_device = None  # () -> the current device's index
-
-
-def _find_device():
-    import torch
-    torch.cuda.current_device()  # initialises torch's side of the GPU
-    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _forget_device():
-    global _device
-    _device = None
-
-
-os.register_at_fork(after_in_child=_forget_device)
-
-
-def _on_current(where: str, *devices: int) -> None:
-    """The calls run on the current device: what lies on another one is refused."""
-    global _device
-    if _device is None:
-        _device = _find_device()
-    current = _device()
-    for d in devices:
-        if d != current:
-            raise ValueError(f"{where}: an argument on device {d}, the current device is {current}")
-
-
-def _space(ws, where: str):
-    """(address, bytes) of a workspace tensor on the current device, or of None."""
-    if ws is not None:
-        _on_current(where, ws.get_device())
-    return _workspace(ws, where)
-
-
 def dr_qgated(x, w: QMatrix, out, act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
     """out = act(x w_gate^T) * (x w_up^T) with w = [w_gate; w_up] and x (2-d float32 or bfloat16) quantized in blocks of
     1 x 128; fast: DR_FAST_SUMS."""
@@ -738,9 +761,12 @@ def dr_qgated(x, w: QMatrix, out, act: int = DR_ACT_SILU, fast: bool = False, wo
     oaddr, okind, orows, ocols, ostep = _dense_rows(out, "dr_qgated out")
     if cols != w.cols or orows != rows or 2 * ocols != w.rows:
         raise ValueError(f"dr_qgated: x {rows} x {cols}, w {w.rows} x {w.cols}, out {orows} x {ocols}")
-    _on_current("dr_qgated", x.get_device(), w.device, out.get_device())
+    device = w.device
+    if not device == x.get_device() == out.get_device():
+        _elsewhere("dr_qgated", x.get_device(), device, out.get_device())
     _check(_lib.dr_qgated(addr, kind, rows, step, w.ref, act, oaddr, okind, ostep, DR_FAST_SUMS if fast else 0,
-                          *_space(workspace, "dr_qgated workspace"), _stream(stream)), "dr_qgated")
+                          *_workspace(workspace, device, "dr_qgated workspace"),
+                          _stream_on(device, stream, "dr_qgated")), "dr_qgated")
 
 
 def dr_qgated_workspace(m: int, w: QMatrix) -> int:
@@ -752,10 +778,12 @@ def dr_qgated_save(x: QMatrix, w: QMatrix, h: QMatrix, gate: QMatrix | None = No
                    act: int = DR_ACT_SILU, fast: bool = False, workspace=None, stream=None) -> None:
     """h = act(x w_gate^T) * (x w_up^T) in 8 bits, and the halves of x w^T as the checkpoint for dr_gated_backward;
     fast: DR_FAST_SUMS."""
-    _on_current("dr_qgated_save", x.device, w.device, h.device, gate.device if gate else h.device,
-                up.device if up else h.device)
+    device = x.device
+    if not device == w.device == h.device or gate and gate.device != device or up and up.device != device:
+        _elsewhere("dr_qgated_save", *[q.device for q in (x, w, h, gate, up) if q])
     _check(_lib.dr_qgated_save(x.ref, w.ref, act, h.ref, gate and gate.ref, up and up.ref, DR_FAST_SUMS if fast else 0,
-                               *_space(workspace, "dr_qgated_save workspace"), _stream(stream)), "dr_qgated_save")
+                               *_workspace(workspace, device, "dr_qgated_save workspace"),
+                               _stream_on(device, stream, "dr_qgated_save")), "dr_qgated_save")
 
 
 def dr_qgated_save_workspace(m: int, w: QMatrix) -> int:
@@ -770,15 +798,19 @@ def dr_gated_backward(dh, gate: QMatrix, up: QMatrix, d: QMatrix | None = None, 
     addr, kind, rows, cols, step = _dense_rows(dh, "dr_gated_backward dh")
     if rows != gate.rows or cols != gate.cols:
         raise ValueError(f"dr_gated_backward: dh {rows} x {cols}, gate {gate.rows} x {gate.cols}")
-    _on_current("dr_gated_backward", dh.get_device(), gate.device, up.device, *[q.device for q in (d, dt, ht) if q])
+    device = gate.device
+    made = [q for q in (d, dt, ht) if q]
+    if not device == up.device == dh.get_device() or any(q.device != device for q in made):
+        _elsewhere("dr_gated_backward", dh.get_device(), *[q.device for q in [gate, up] + made])
     _check(_lib.dr_gated_backward(addr, kind, step, gate.ref, up.ref, act, d and d.ref, dt and dt.ref, ht and ht.ref,
-                                  _stream(stream)), "dr_gated_backward")
+                                  _stream_on(device, stream, "dr_gated_backward")), "dr_gated_backward")
 
 
 def dr_qtranspose(src: QMatrix, qt: QMatrix, stream=None) -> None:
     """qt = the transpose of src, quantized anew in blocks of 1 x 128."""
-    _on_current("dr_qtranspose", src.device, qt.device)
-    _check(_lib.dr_qtranspose(src.ref, qt.ref, _stream(stream)), "dr_qtranspose")
+    if src.device != qt.device:
+        _elsewhere("dr_qtranspose", src.device, qt.device)
+    _check(_lib.dr_qtranspose(src.ref, qt.ref, _stream_on(src.device, stream, "dr_qtranspose")), "dr_qtranspose")
 
 
 # ------------------------------------------------------------------ gradients

@@ -141,7 +141,7 @@ __device__ __forceinline__ u32x2 load_codes8(const QView& q, uint32_t row, uint3
   return __builtin_bit_cast(u32x2, ahead < 8 ? w >> 8 * ahead : 0ull);
 }
 
-// Any f: a workgroup takes one tile of d's 2f columns.  A lane's 8 columns begin anywhere in a block of gate or up, so that
+// Any f: a workgroup takes one tile of d's 2f columns, or, for ht alone, of its f.  A lane's 8 columns begin anywhere in a block of gate or up, so that
 // they may have two scales; where gate's half ends among them, up's first columns follow (ODD: f no multiple of 8, else neither
 // comes about).  Rows of fewer than 8 are read element by element.  2000 x 2000 in 16.3 us; element by element 23.5.
 template <bool BF16, bool SILU, bool ODD>
@@ -242,7 +242,7 @@ hipError_t launch_gated_backward(const GatedBackward& l, hipStream_t st) {
   BackwardArgs a = {l.dh, l.dh_stride, l.rows, l.f, 0, 0, 0, 0, l.act, l.gate, l.up, l.d, l.dt, l.ht};
   const dim3 block(kTileLanes);
   const bool silu = l.act.k3 == 0, whole = l.f % kBlock == 0 && l.dh_stride * (l.dh_bf16 ? 2 : 4) < 1 << 24;
-  a.tiles_x = (uint32_t)(whole ? l.f / kBlock : ceil_div(2 * (int64_t)l.f, kBlock));
+  a.tiles_x = (uint32_t)ceil_div(whole || !(l.d.data || l.dt.data) ? l.f : 2 * (int64_t)l.f, kBlock);
   a.tiles = a.tiles_x * (uint32_t)ceil_div(l.rows, 128);
   // where the CUs hold every matrix of every tile at once, each is computed by a workgroup of its own: 1024 x 1024 in 6.3 us, by one
   // workgroup a tile 8.4

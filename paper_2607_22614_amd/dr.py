@@ -779,7 +779,7 @@ def dr_qgated_save(x: QMatrix, w: QMatrix, h: QMatrix, gate: QMatrix | None = No
     """h = act(x w_gate^T) * (x w_up^T) in 8 bits, and the halves of x w^T as the checkpoint for dr_gated_backward;
     fast: DR_FAST_SUMS."""
     device = x.device
-    if not device == w.device == h.device or gate and gate.device != device or up and up.device != device:
+    if not device == w.device == h.device == (gate or x).device == (up or x).device:
         _elsewhere("dr_qgated_save", *[q.device for q in (x, w, h, gate, up) if q])
     _check(_lib.dr_qgated_save(x.ref, w.ref, act, h.ref, gate and gate.ref, up and up.ref, DR_FAST_SUMS if fast else 0,
                                *_workspace(workspace, device, "dr_qgated_save workspace"),
@@ -799,9 +799,8 @@ def dr_gated_backward(dh, gate: QMatrix, up: QMatrix, d: QMatrix | None = None, 
     if rows != gate.rows or cols != gate.cols:
         raise ValueError(f"dr_gated_backward: dh {rows} x {cols}, gate {gate.rows} x {gate.cols}")
     device = gate.device
-    made = [q for q in (d, dt, ht) if q]
-    if not device == up.device == dh.get_device() or any(q.device != device for q in made):
-        _elsewhere("dr_gated_backward", dh.get_device(), *[q.device for q in [gate, up] + made])
+    if not device == up.device == dh.get_device() == (d or gate).device == (dt or gate).device == (ht or gate).device:
+        _elsewhere("dr_gated_backward", dh.get_device(), *[q.device for q in (gate, up, d, dt, ht) if q])
     _check(_lib.dr_gated_backward(addr, kind, step, gate.ref, up.ref, act, d and d.ref, dt and dt.ref, ht and ht.ref,
                                   _stream_on(device, stream, "dr_gated_backward")), "dr_gated_backward")
 

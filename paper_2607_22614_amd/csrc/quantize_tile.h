@@ -1,5 +1,5 @@
-// Quantization of a tile of 128 x 128 elements that a workgroup holds in registers: shared by the kernels that quantize
-// (quantize.hip) and those that compute what they quantize (gated_backward.hip).
+// Quantization of a tile of 128 x 128 elements that a workgroup holds in registers as they lie in memory (quantize.hip), and what
+// it has in common with that of computed values (quantize_values.h): the places of tiles and lanes, and the scale codes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -49,10 +49,9 @@ __device__ __forceinline__ TilePlace tile_place(uint32_t tiles_x) { return place
 // into qt, whose rows are q's columns (COLS).  SQUARE: one scale for the tile, else one per row (DPP) and one per column (over
 // the four rows of lanes, then over the waves in LDS).  The transpose's codes are packed 4 rows to a word, turned in LDS (one
 // 128-byte row per column, its words spread by an exclusive or over the banks), and leave as whole 128-byte rows.
-//   A second call with COLS may follow in the same space: the barrier behind its maxima stands between the first one's reads
-// of `turned` and its own writes, and the first one's last barrier behind all reads of `cmax`.
-template <bool BF16, bool SQUARE, bool ROWS, bool COLS, class Space>
-__device__ __forceinline__ void quantize_tile(const Raw8<BF16> (&v)[kTileRows], const TilePlace& at, const QView& q, const QView& qt, Space& space) {
+template <bool BF16, bool SQUARE, bool ROWS, bool COLS>
+__device__ __forceinline__ void quantize_tile(const Raw8<BF16> (&v)[kTileRows], const TilePlace& at, const QView& q, const QView& qt,
+                                              TileSpace<COLS>& space) {
   constexpr int R = kTileRows, kWaves = kTileWaves;
   const uint32_t rows = ROWS ? q.rows : qt.cols, cols = ROWS ? q.cols : qt.rows;
   const uint32_t tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, wave = tid / 64;

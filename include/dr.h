@@ -673,8 +673,11 @@ int dr_qgated_save_workspace(int64_t m, int64_t f, int64_t k, uint64_t* bytes);
  *   dt = its transpose (2F x M), and
  *   ht = the transpose of act(gate) * up (F x M), again from the checkpoint,
  * each in 8 bits in blocks of 1 x 128, as dr_quantize gives it from the fp32
- * values.  Any of d, dt and ht may be NULL, but not all; F a multiple of 128 reads
- * its inputs once (rows of dh less than 2^24 bytes apart), another F twice.
+ * values.  dh * up is formed first: where it passes fp32's largest number, dgate
+ * becomes NaN, also where act' would bring it back.  Any of d, dt and ht may be
+ * NULL, but not all (dh is read for ht alone too).  F a multiple of 128 (rows of dh
+ * less than 2^24 bytes apart) reads its inputs once, another F twice, and small
+ * calls, which leave CUs free, once more for each result.
  * Errors: DR_EINVAL (limits above, shapes that differ, block_rows, null or
  * misaligned pointers, 2^23 or more tiles of 128 x 128), DR_EHIP. */
 int dr_gated_backward(const void* dh, int32_t dh_type, int64_t dh_row_stride, const dr_qmatrix* gate,

@@ -108,8 +108,9 @@ int product_and_join(ProductLaunch l, GatedJoin& j, uint8_t* sums, Act act, hipS
 // Beyond kFusedRows rows of x a launch of its own quantizes them, which takes 2 us between others and, with the host's calls for
 // two launches, 8.5 at least; in the product's kernel, where every workgroup quantizes what it reads, x costs 1.5 and a tenth
 // of the product, in fp32 1.8 and seven tenths.  In us, apart / in the product's kernel, launched by the host: 333 x 344 x 256
-// fp32 8.8 / 6.9, bf16 8.4 / 6.2; 100 x 1000 x 1000 8.9 / 6.3; 32 x 4864 x 896 8.6 / 7.1; 61 x 4864 x 896 10.0 / 10.5; 20 x 3584 x
-// 4096 11.8 / 12.7; 40 x 2000 x 2000 8.6 / 9.4.  With 64 instead of 32 rows a workgroup the latter lose 10 to 50 %.
+// fp32 9.0 / 7.3, bf16 9.0 / 6.5; 100 x 1000 x 1000 8.7 / 7.0; 32 x 4864 x 896 8.9 / 7.6; 61 x 4864 x 896 10.5 / 10.9; 20 x 3584 x
+// 4096 13.1 / 13.2; 40 x 2000 x 2000 9.2 / 9.9 (profiles/gated_plans.txt: 32 shapes, the choice at most 2 % above the better one).
+// With 64 instead of 32 rows a workgroup the latter lose 10 to 50 %.
 GatedRowsPlan plan_gated_rows(int64_t m, int64_t f, int64_t k, bool x_bf16, bool fast) {
   const int64_t kb = ceil_div(k, kBlock);
   const GatedRowsPlan plan{m <= kFusedRows, plan_product(m, 2 * f, kb, fast)};
@@ -119,10 +120,11 @@ GatedRowsPlan plan_gated_rows(int64_t m, int64_t f, int64_t k, bool x_bf16, bool
   return inside < apart ? GatedRowsPlan{true, {ProductPlan::kDirect, 1, 0, 2, inside}} : plan;
 }
 
-// Times in us as plan_product's: a step of a tile of 256 rows takes 1.34 (exact sums 2.7), of 128 rows, alone on its CU, 0.85 (1.5);
-// what a tile costs beside its steps is 12 and 7, the codes' part of it included; a second launch 6.  As a product with fp32 sums: that
-// product, a launch of 4, and the sums' and results' 20 bytes an element of h and split at 6.5 TB/s.  In us, by sums / 128 / 256
-// rows a tile: 200 x 688 x 256 7.2 / 10.1 / 15.4; 700 x 4864 x 896 26 / 15 / 22; 512 x 3456 x 5120 33 / 49 / 63; 2048 x 3456 x 5120 80 / 93 / 68.
+// Times in us as plan_product's: a step of a tile of 256 rows takes 1.34 (exact sums 2.7), of 128 rows, alone on its CU,
+// 0.85 (1.5); what a tile costs beside its steps is 12 and 7, the codes' part of it included; a second launch 6.  As a product
+// with fp32 sums: that product, a launch of 4, and the sums' and results' 20 bytes an element of h and split at 6.5 TB/s.  In us,
+// by sums / 128 / 256 rows a tile: 200 x 688 x 256 7.7 / 10.4 / 15.8; 700 x 4864 x 896 27 / 17 / 23; 512 x 3456 x 5120 33 / 49 / 64;
+// 2048 x 3456 x 5120 99 / 124 / 83 (profiles/gated_plans.txt: 20 shapes, the choice at most 2 % above the best way).
 GatedCodesPlan plan_gated_codes(int64_t m, int64_t f, int64_t kb, bool fast) {
   const ProductPlan sums = plan_product(m, 2 * f, kb, fast);
   if (m <= 32 || !kb) return {0, 0, sums};

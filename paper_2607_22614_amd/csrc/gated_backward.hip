@@ -23,8 +23,8 @@ struct BackwardArgs {
   QView gate, up, d, dt, ht;
 };
 
-// Bands of sixteen tiles down, a contiguous eighth of them to each XCD: 8192 x 14336 in 218 us, in the order of dr_quantize's
-// tiles 226 (bands of 8 and 32: 229, 219).
+// Bands of sixteen tiles down, a contiguous eighth of them to each XCD: 8192 x 14336 in 218 us as first measured, in the order of
+// dr_quantize's tiles 226 (bands of 8 and 32: 229, 219).
 __device__ __forceinline__ TilePlace backward_place(const BackwardArgs& p) { return place_of<16>(xcd_tile(blockIdx.x % p.tiles, p.tiles), p.tiles, p.tiles_x); }
 
 __device__ __forceinline__ uint32_t scale_at(const QView& q, uint32_t row, uint32_t block) {
@@ -51,9 +51,10 @@ __device__ __forceinline__ void pin(Raw8<BF16> (&r)[N]) {
     for (int h = 0; h < (BF16 ? 1 : 2); ++h) asm volatile("" : "+v"(r[i].w[h]));
 }
 
-// f a multiple of 128, rows of dh less than 2^24 bytes apart: gate's and up's halves of d consist of whole tiles, and a workgroup takes one of either.  dup and h are
-// computed when dgate has left: all three at once would take the registers of a second workgroup (8192 x 14336 341 us with them).
-//   Memory-bound: 8192 x 14336 in 218 us, 4.9 TB/s, with the vector units busy 60 % of the time.
+// f a multiple of 128, rows of dh less than 2^24 bytes apart: gate's and up's halves of d consist of whole tiles, and a workgroup
+// takes one of either.  dup and h are computed when dgate has left: all three at once would take the registers of a second
+// workgroup (8192 x 14336 341 us with them).
+//   Memory-bound: 8192 x 14336 in 219 us, 4.9 TB/s, with the vector units busy 65 % of the time.
 template <bool BF16, bool SILU>
 __global__ __launch_bounds__(kTileLanes, 4) void gated_backward_kernel(BackwardArgs p) {
   __shared__ ValuesSpace space;
@@ -141,9 +142,10 @@ __device__ __forceinline__ u32x2 load_codes8(const QView& q, uint32_t row, uint3
   return __builtin_bit_cast(u32x2, ahead < 8 ? w >> 8 * ahead : 0ull);
 }
 
-// Any f: a workgroup takes one tile of d's 2f columns, or, for ht alone, of its f.  A lane's 8 columns begin anywhere in a block of gate or up, so that
-// they may have two scales; where gate's half ends among them, up's first columns follow (ODD: f no multiple of 8, else neither
-// comes about).  Rows of fewer than 8 are read element by element.  2000 x 2000 in 16.3 us; element by element 23.5.
+// Any f: a workgroup takes one tile of d's 2f columns, or, for ht alone, of its f (2000 x 2000 7.7 us; of 2f 12.0).  A lane's 8
+// columns begin anywhere in a block of gate or up, so that they may have two scales; where gate's half ends among them, up's
+// first columns follow (ODD: f no multiple of 8, else neither comes about).  Rows of fewer than 8 are read element by element.
+// 2000 x 2000 in 16.7 us; element by element 23.5.
 template <bool BF16, bool SILU, bool ODD>
 __global__ __launch_bounds__(kTileLanes) void gated_backward_any_kernel(BackwardArgs p) {
   __shared__ ValuesSpace space;

@@ -279,7 +279,9 @@ void launch_direct(ArgsOf<RESULTS> a, hipStream_t st) {
 // workgroup reads: 6912 x 5120 take 9.3 us for one row.  More blocks in flight per wave (2 to 6) lost 5 to 50 %.
 template <int TT, int X, int RESULTS>
 void launch_few_rows(const ArgsOf<RESULTS>& a, hipStream_t st) {
-  // pairs: two tiles as long as all of them run at once (16 rows of x, 4600 pairs of 8192 columns: 31.4 us with two, 24.9 with four)
+  // pairs: more tiles as soon as not all of them run at once.  In us, 1 / 2 / 4 tiles, 16 rows of x (2 rows): 2000 pairs of 4096
+  // columns 9.5 / 11.2 / 15.0 (7.2 / 8.9 / 12.7), 2200 14.8 / 11.2 / 14.8 (10.6 / 8.9 / 12.6), 4000 14.7 / 11.6 / 15.1 (10.8 / 10.4 / 12.7),
+  // 4600 of 8192 37 / 35 / 28 (24.5 / 26.8 / 26.4, the most that the rule loses but for 14336 of 4096, 34 / 28 / 31: 8 %)
   const uint32_t columns16 = RESULTS == kSums ? direct_columns16(a.n) : a.n <= 2048 ? 1 : a.n <= 4096 ? 2 : 4;
   if (columns16 == 1) launch_direct<1, TT, direct_waves(1), X, RESULTS>(a, st);
   else if (columns16 == 2) launch_direct<2, TT, direct_waves(2), X, RESULTS>(a, st);
@@ -449,8 +451,8 @@ __device__ __forceinline__ float here(float v) {
 // Results of a wave in 8 bits: of TM * 32 rows, TN / 2 * 32 columns of gate, up and h each, half a block of 128.  A row's largest
 // magnitudes go to the wave beside it, which has the block's other half, through the waves' own LDS (`mine` and `other`,
 // TN * 2 KiB each, two places in turn, so that one barrier for each 32 rows is enough); then the codes are turned there and
-// leave 64 bytes of a row at a time; 6 us of a tile of 256 x 256, the vector units' time.  As above without branches: what lies outside of a matrix, and a matrix that is
-// not wanted, are beyond their buffers' ends.
+// leave 64 bytes of a row at a time; 6 us of a tile of 256 x 256, the vector units' time.  As above without branches: what lies
+// outside of a matrix, and a matrix that is not wanted, are beyond their buffers' ends.
 constexpr uint32_t kCodesRow = 64, kMaxima = 3 * 32 * kCodesRow;
 template <int TM, int TN>
 __device__ __forceinline__ void store_codes(const GatedArgs& p, const f32x16 (&acc)[TN][TM], uint8_t* mine, const uint8_t* other, uint32_t m0, uint32_t f0,
@@ -557,11 +559,11 @@ __device__ __forceinline__ void store_codes(const GatedArgs& p, const f32x16 (&a
 // blocks ahead, and the scale codes come with them, a word (four blocks' codes) per row: loaded to registers they would have
 // to wait for the copies before them.
 //   kGated, kGatedCodes: b's rows of a stage are 32 of gate's and the same 32 of up's in turn, so that a lane's sums of either
-// stand in the same places of two of its accumulators, and a tile is BN / 2 columns of c.  8192 x 3456 pairs x 5120 take 227 us
-// (the sums of all 6912 rows as bf16 225), as codes with gate and up 250; 8192 x 14336 pairs x 4096 as codes 810 to 835 (773).
-//   Long products are bound by power: 8192 x 14336 x 4096 take 385 us (2500 TFLOP/s; 410 on a card that gets less) with the matrix units busy 64 % of the
-// cycles at a clock of about 1.8 GHz, exact sums 700 to 750 us.  Few rows are bound by how fast b comes: 61 x 151936 x 896
-// 36 us (4.7 TB/s); short K by the start and end of tiles: 768 x 9728 x 896 13 us.
+// stand in the same places of two of its accumulators, and a tile is BN / 2 columns of c.  8192 x 3456 pairs x 5120 take 228 us
+// (the sums of all 6912 rows as bf16 225), as codes with gate and up 283; 8192 x 14336 pairs x 4096 as codes 820 to 845 (773).
+//   Long products are bound by power: 8192 x 14336 x 4096 take 385 us (2500 TFLOP/s; 410 on a card that gets less) with the
+// matrix units busy 64 % of the cycles at a clock of about 1.8 GHz, exact sums 700 to 750 us.  Few rows are bound by how fast b
+// comes: 61 x 151936 x 896 36 us (4.7 TB/s); short K by the start and end of tiles: 768 x 9728 x 896 13 us.
 template <int BM, int BN, int WM, int WN, int BYTES, bool VEC, bool FAST, bool ONE, int S, int RESULTS>
 __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESULTS> p) {
   constexpr bool PAIRS = RESULTS != kSums, CODES = RESULTS == kGatedCodes;
@@ -596,7 +598,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
   for (int i = 0; i < TM; ++i) acode[i] = 4 * ((wm + i * 32 + r) >> p.a.sh);
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
-    if constexpr (PAIRS) bcode[i] = pair_of(wn + i * 32 + r) + second_of(wn + i * 32) * p.half;  // the row itself: up's first one may lie inside a square block
+    // the row itself: up's first one may lie inside a square block
+    if constexpr (PAIRS) bcode[i] = pair_of(wn + i * 32 + r) + second_of(wn + i * 32) * p.half;
     else bcode[i] = 4 * ((wn + i * 32 + r) >> p.b.sh);
   }
   const Buffer ascales = buffer_at(p.a.scales, (p.kb + 3) / 4 * p.a.srows * 4), bscales = buffer_at(p.b.scales, (p.kb + 3) / 4 * p.b.srows * 4);
@@ -806,8 +809,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile_kernel(ArgsOf<RESUL
 }
 
 // Workgroups with a CU to themselves stage four blocks, in the LDS of the second one that is not there: fast sums of 512 x
-// 6912 x 5120 in 24 us instead of 35 (up to 31 where less of it lies in the last cache), 100 x 32064 x 4096 37 (46), 2048 x 2000 x 2000 14 (17).  Exact sums are not faster (512 x
-// 896 x 4864 20.6 and 19.9), nor are items of two or three blocks (200 x 688 x 256 5.7 and 5.4).
+// 6912 x 5120 in 24 us instead of 35 (up to 31 where less of it lies in the last cache), 100 x 32064 x 4096 37 (46), 2048 x 2000 x 2000
+// 14 (17).  Exact sums are not faster (512 x 896 x 4864 20.6 and 19.9), nor are items of two or three blocks (200 x 688 x 256 5.7 and 5.4).
 constexpr uint32_t kCus = 256;
 constexpr int kDeep = 4;
 template <int BM, int BN, int BYTES, bool VEC, bool ONE, int RESULTS>

@@ -604,13 +604,17 @@ def _elsewhere(where: str, *devices: int) -> None:
 
 
 def _stream_on(device: int, stream, where: str) -> int:
-    """The stream's handle, for a call with arguments on `device`: the calls run on the current one."""
+    """The stream's handle, for a call with arguments on `device`: the calls run on the current one, on a stream of its own."""
     current = _device()
     if device != current:
         _elsewhere(where, device)
     if stream is None:
         return _raw_stream(current)
-    return stream if isinstance(stream, int) else stream.cuda_stream
+    if isinstance(stream, int):
+        return stream
+    if stream.device_index != current:
+        raise ValueError(f"{where}: a stream of device {stream.device_index}, the current device is {current}")
+    return stream.cuda_stream
 
 
 _TYPES: dict = {}  # torch dtype -> DR_TYPE_*, filled at the first tensor

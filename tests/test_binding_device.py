@@ -96,3 +96,12 @@ def test_codes_and_scales_lie_together():
     with pytest.raises(ValueError, match="device"):
         _codes(3, 200, 0, 1)
     assert _codes(3, 200, 1, 1).device == 1
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_a_stream_of_another_device(current, monkeypatch):
+    monkeypatch.setattr(dr, "_device", lambda: current)
+    streams = [types.SimpleNamespace(device_index=i, cuda_stream=77 + i) for i in range(2)]
+    assert dr._stream_on(current, streams[current], "here") == 77 + current
+    with pytest.raises(ValueError, match="current device"):
+        dr._stream_on(current, streams[1 - current], "here")
